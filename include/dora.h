@@ -239,6 +239,59 @@ dora_status dora_decode_attn_grouped(const dora_decode_desc* desc, const void* q
                                      int32_t* shared_pages_out, void* workspace,
                                      size_t workspace_bytes, dora_stream_t stream);
 
+/* Decode attention for a tree of drafted tokens per sequence (verification of
+ * speculative drafts): num_nodes query rows of a sequence share one pass over its
+ * cached tokens.  With T = num_nodes, n = node_counts[b] (T without node_counts) and
+ * L = seq_lens[b], for every node i < n and query head h, g = h / G:
+ *   s_t   = sm_scale * <q[b][i][h], K_t>              t < L (the cache, as above)
+ *   s'_j  = sm_scale * <q[b][i][h], k_draft[b][j][g]>  j < n with bit j of
+ *                                                     tree_mask[b][i] set
+ *   out[b][i][h] = softmax over all of them, applied to V_t and v_draft[b][j][g]
+ * A node that sees nothing (L = 0 and no bit) gives 0; rows of nodes i >= n are left
+ * as they were.  The mask is taken as it is: a node that attends itself has its own
+ * bit set, and bits of nodes >= n count as 0.  The drafts' K and V are not in the
+ * cache (a rejected draft leaves no trace in the pages or their scales); store what
+ * is accepted with dora_kv_append_path.
+ *   desc         as for dora_decode_attn; seq_lens counts the cached tokens only;
+ *                num_waves (0 = library default) is rounded up to workgroups of 4,
+ *                min_range_pages is not used
+ *   num_nodes    T in [1, 64]
+ *   q, out       device bf16 [B][T][Hq][d]
+ *   k_draft, v_draft  device bf16 [B][T][Hkv][d], 16-byte aligned
+ *   tree_mask    device uint64 [B][T]
+ *   node_counts  device int32 [B] in [0, T], or NULL (all T; values outside are
+ *                taken as the nearest inside)
+ *   workspace    >= dora_decode_tree_workspace_bytes(desc, num_nodes) bytes
+ * Other arguments, flags and errors as for dora_decode_attn.  Repeated calls on the
+ * same inputs and device are bitwise identical. */
+size_t dora_decode_tree_workspace_bytes(const dora_decode_desc* desc, int32_t num_nodes);
+dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_nodes, const void* q,
+                                  const void* k_draft, const void* v_draft,
+                                  const uint64_t* tree_mask, const int32_t* node_counts,
+                                  const void* k_pages, const void* v_pages,
+                                  const int32_t* block_table, const int32_t* seq_lens,
+                                  const int32_t* version_ids, void* out, void* workspace,
+                                  size_t workspace_bytes, dora_stream_t stream);
+
+/* Decode attention with a sliding window and sinks: the operation of
+ * dora_decode_attn over the tokens t < L of sequence b with
+ *   t < sinks  or  t >= L - window
+ * alone.  Only the pages that hold such tokens are read, and only their table entries:
+ * the others may hold anything (dora_pool_release_window frees their pages).
+ *   window       >= 1 (the newest token counts among them)
+ *   sinks        >= 0
+ *   desc         as for dora_decode_attn; num_waves and min_range_pages are not used;
+ *                DORA_FLAG_VALIDATE checks the entries that are read
+ *   workspace    >= dora_decode_window_workspace_bytes(desc, window, sinks) bytes
+ * Other arguments, flags and errors as for dora_decode_attn. */
+size_t dora_decode_window_workspace_bytes(const dora_decode_desc* desc, int32_t window,
+                                          int32_t sinks);
+dora_status dora_decode_attn_window(const dora_decode_desc* desc, int32_t window, int32_t sinks,
+                                    const void* q, const void* k_pages, const void* v_pages,
+                                    const int32_t* block_table, const int32_t* seq_lens,
+                                    const int32_t* version_ids, void* out, void* workspace,
+                                    size_t workspace_bytes, dora_stream_t stream);
+
 /* Store every sequence's current-token K and V into its page slot: the write
  * that precedes each decode step (the per-token step of Sec. 2.2; seq_lens
  * counts that token, so dora_decode_attn with the same seq_lens then attends
@@ -278,6 +331,32 @@ dora_status dora_kv_append(const dora_decode_desc* desc, const void* k_new, cons
                            const int32_t* version_ids, void* k_pages, void* v_pages,
                            float* k_scales, float* v_scales, int32_t* dev_status,
                            dora_stream_t stream);
+
+/* Store several tokens of every sequence: the accepted path of a tree of drafts, or a
+ * run of a prompt.  With n = counts[b] (num_tokens without counts) and L =
+ * seq_lens[b], which counts them, token i < n is row path[b][i] (row i without path) of
+ * k_new[b] and v_new[b] and goes to position L - n + i.  The pages and scales end up as
+ * after n calls of dora_kv_append, one token each in that order, bit for bit.
+ *   num_tokens   T in [1, DORA_PATH_MAX_TOKENS], rows of k_new and v_new per sequence
+ *   k_new, v_new device bf16 [B][T][Hkv][d], 16-byte aligned
+ *   path         device int32 [B][T] or NULL; entries i >= n are not read; an index
+ *                may occur more than once
+ *   counts       device int32 [B] in [0, T] or NULL
+ *   dev_status   device int32 or NULL: receives DORA_OK, or DORA_ERR_DEVICE_CHECK if
+ *                something was skipped: a sequence whose n is negative or above T or L,
+ *                or whose length exceeds its block-table row; a page whose id is out of
+ *                range (or, under DORA_FLAG_VALIDATE with desc->page_owner, another
+ *                version's); a page with a token whose path entry is no row.  A skipped
+ *                sequence or page is left as it was; no write ever leaves the pool.
+ * Other arguments as for dora_kv_append.  Enqueued on `stream`; one launch (two with
+ * dev_status). */
+#define DORA_PATH_MAX_TOKENS (1 << 19)
+dora_status dora_kv_append_path(const dora_decode_desc* desc, int32_t num_tokens,
+                                const void* k_new, const void* v_new, const int32_t* path,
+                                const int32_t* counts, const int32_t* block_table,
+                                const int32_t* seq_lens, const int32_t* version_ids, void* k_pages,
+                                void* v_pages, float* k_scales, float* v_scales,
+                                int32_t* dev_status, dora_stream_t stream);
 
 /* ---------------------------------------------------------------------------
  * KV page pack / unpack: the device half of the paper's two-phase state
@@ -349,6 +428,19 @@ dora_status dora_kv_page_unpack(const dora_pack_desc* desc, int32_t src_version,
                                 float* k_scales, float* v_scales,
                                 int32_t* dev_status, dora_stream_t stream);
 
+/* Copy pages inside one pool: page dst_pages[i] becomes a copy of page src_pages[i]
+ * (K, V and, for fp8, its scales), bit for bit, for i < n_pages (device int32 lists).
+ * The device half of dora_pool_fork_seq and dora_pool_compact, which make the lists.
+ * A page may be copied to many places, and onto itself (nothing happens); the
+ * destinations must differ from each other, and none may be the source of another
+ * copy.  desc->policy_version and n_seqs are not used.  dev_status (device int32 or
+ * NULL) receives DORA_OK, or DORA_ERR_DEVICE_CHECK if a pair was skipped because one
+ * of its ids is out of range. */
+dora_status dora_kv_page_copy(const dora_pack_desc* desc, void* k_pages, void* v_pages,
+                              float* k_scales, float* v_scales, const int32_t* src_pages,
+                              const int32_t* dst_pages, int64_t n_pages, int32_t* dev_status,
+                              dora_stream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Orchestrator planners (host, integer arithmetic; Sec. 3.3).  Versions are
  * indexed oldest first; the last index is the latest version.
@@ -400,23 +492,25 @@ dora_status dora_pool_add_seq(dora_pool* pool, int32_t version, int32_t num_toke
                               int64_t* seq_id_out);
 /* Grow a sequence to new_num_tokens (>= current), allocating pages as needed. */
 dora_status dora_pool_extend_seq(dora_pool* pool, int64_t seq_id, int32_t new_num_tokens);
-/* Release a sequence and all of its pages. */
+/* Release a sequence; its pages are free once no other sequence holds them. */
 dora_status dora_pool_free_seq(dora_pool* pool, int64_t seq_id);
 /* Tokens, version and page count of a sequence (any out pointer may be NULL). */
 dora_status dora_pool_seq_info(const dora_pool* pool, int64_t seq_id, int32_t* num_tokens,
                                int32_t* version, int32_t* num_pages);
-/* Copy a sequence's page ids in logical order into pages_out[cap]. */
+/* Copy a sequence's page ids in logical order into pages_out[cap]; -1 stands for a
+ * page that dora_pool_release_window has released. */
 dora_status dora_pool_seq_pages(const dora_pool* pool, int64_t seq_id,
                                 int32_t* pages_out, int32_t cap, int32_t* n_out);
-/* Fill host arrays for a decode batch: table_out[n][stride] (unused entries
- * set to 0), lens_out[n], versions_out[n].  INVALID_ARG if a sequence needs
+/* Fill host arrays for a decode batch: table_out[n][stride] (entries that are unused,
+ * or whose page is released, set to 0), lens_out[n], versions_out[n].  INVALID_ARG if a sequence needs
  * more than `stride` pages. */
 dora_status dora_pool_block_table(const dora_pool* pool, const int64_t* seq_ids, int32_t n,
                                   int32_t stride, int32_t* table_out, int32_t* lens_out,
                                   int32_t* versions_out);
 /* owner_out[num_pages]: owning version of each page, -1 if free. */
 dora_status dora_pool_page_owner(const dora_pool* pool, int16_t* owner_out);
-/* Pages held by `version` (version = -1: all versions) and pages free. */
+/* Pages held by `version` (version = -1: all versions; a page that several sequences
+ * share counts once) and pages free. */
 dora_status dora_pool_stats(const dora_pool* pool, int32_t version, int64_t* pages_used,
                             int64_t* pages_free);
 /* Migrate a sequence from `src` to `dst` (same-version instances): allocates
@@ -426,11 +520,38 @@ dora_status dora_pool_stats(const dora_pool* pool, int32_t version, int64_t* pag
  * sequence's version (DORA_ERR_VERSION_MISMATCH otherwise).  If src == dst the
  * sequence stays where it is (locality: no pages move, n_out = 0 and
  * dst_seq_id = seq_id).  The source sequence is kept until the caller frees it
- * after the copy. */
+ * after the copy.  Pages shared with other sequences are copied for the migrated one;
+ * released pages stay released. */
 dora_status dora_pool_migrate_seq(dora_pool* src, int64_t seq_id, dora_pool* dst,
                                   int32_t dst_version, int64_t* dst_seq_id,
                                   int32_t* src_pages, int32_t* dst_pages, int32_t cap,
                                   int32_t* n_out);
+
+/* Fork a sequence: register a new one, of the same version, that holds the first
+ * num_tokens tokens (0 <= num_tokens <= the sequence's; all of them where the sequence
+ * has released pages, else DORA_ERR_INVALID_ARG).  It shares the pages that these
+ * fill, and gets a page of its own for the last, partly filled one: then *n_out = 1 and
+ * the page must be copied from *src_page to *dst_page with dora_kv_page_copy before
+ * either sequence is appended to (n_out = 0: nothing to copy; released pages stay
+ * released).  Shared pages are what dora_decode_attn_grouped reads once.
+ * DORA_ERR_POOL_EXHAUSTED leaves the pool unchanged. */
+dora_status dora_pool_fork_seq(dora_pool* pool, int64_t seq_id, int32_t num_tokens,
+                               int64_t* new_seq_id, int32_t* src_page, int32_t* dst_page,
+                               int32_t* n_out);
+/* Release the pages of a sequence that no later dora_decode_attn_window call with this
+ * window and these sinks reads (window >= 1, sinks >= 0): those that lie whole between
+ * the sinks and the window of the newest token.  Its tokens still count, its table keeps
+ * its width; it is for dora_decode_attn_window from then on.  *n_out (may be NULL): pages released by this sequence in this call. */
+dora_status dora_pool_release_window(dora_pool* pool, int64_t seq_id, int32_t window,
+                                     int32_t sinks, int32_t* n_out);
+/* Move live pages from the pool's end into its free places, so that the n live pages
+ * are pages 0 .. n - 1: fills src_pages and dst_pages (cap entries; *n_out of them) for
+ * one dora_kv_page_copy per layer and renames the pages in every sequence; block tables
+ * taken before are stale.  Afterwards pages are handed out in increasing order.
+ * DORA_ERR_WORKSPACE_TOO_SMALL (more than cap moves; *n_out says how many) leaves the
+ * pool unchanged. */
+dora_status dora_pool_compact(dora_pool* pool, int32_t* src_pages, int32_t* dst_pages, int32_t cap,
+                              int32_t* n_out);
 
 #ifdef __cplusplus
 }

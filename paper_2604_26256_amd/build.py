@@ -22,9 +22,9 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdora.so")
 ARCH = "gfx950"
 
-HIP_SOURCES = ["decode.hip", "segment.hip", "pack.hip", "append.hip", "grouped.hip", "measure.hip",
-               "noalloc.hip"]
-CXX_SOURCES = ["api.cpp", "pool.cpp", "plan.cpp"]
+HIP_SOURCES = ["tree.hip", "window.hip", "decode.hip", "segment.hip", "pack.hip", "append.hip",
+               "append_path.hip", "page_copy.hip", "grouped.hip", "measure.hip", "noalloc.hip"]
+CXX_SOURCES = ["api.cpp", "cache_api.cpp", "pool.cpp", "plan.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

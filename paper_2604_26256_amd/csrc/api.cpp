@@ -30,6 +30,10 @@ bool geometry_supported(const dora_decode_desc& d) {
          seqs * d.block_table_stride * d.num_kv_heads < ((int64_t)1 << 31);
 }
 
+}  // namespace
+
+namespace dora {
+
 // Host-checkable validity of a descriptor (pointers are checked separately).
 dora_status check_desc(const dora_decode_desc* d) {
   if (!d) return DORA_ERR_INVALID_ARG;
@@ -41,6 +45,10 @@ dora_status check_desc(const dora_decode_desc* d) {
   if (!geometry_supported(*d)) return DORA_ERR_UNSUPPORTED;
   return DORA_OK;
 }
+
+}  // namespace dora
+
+namespace {
 
 // Longest row, in tokens, that the segment kernel takes whole.
 constexpr int kWholeMost = 2048;
@@ -570,7 +578,11 @@ dora_status dora_kv_append(const dora_decode_desc* desc, const void* k_new, cons
 // pack / unpack
 // ---------------------------------------------------------------------------
 
-static dora_status check_pack_desc(const dora_pack_desc* d) {
+}  // extern "C"
+
+namespace dora {
+
+dora_status check_pack_desc(const dora_pack_desc* d) {
   if (!d) return DORA_ERR_INVALID_ARG;
   if (d->num_kv_heads < 1 || d->page_size < 1 || d->head_dim < 1 || d->num_pages < 1)
     return DORA_ERR_INVALID_ARG;
@@ -581,6 +593,10 @@ static dora_status check_pack_desc(const dora_pack_desc* d) {
     return DORA_ERR_UNSUPPORTED;
   return DORA_OK;
 }
+
+}  // namespace dora
+
+extern "C" {
 
 size_t dora_kv_packed_bytes(const dora_pack_desc* desc, int64_t n_pages) {
   if (check_pack_desc(desc) != DORA_OK || n_pages < 0) return 0;

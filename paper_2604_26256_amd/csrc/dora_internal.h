@@ -38,6 +38,10 @@ struct WsLayout {
 // (desc->num_waves if set).  Falls back to a 256-CU, 8-wave estimate when no
 // device can be queried.
 int64_t decode_waves(const dora_decode_desc& d);
+// Host-checkable validity of a descriptor.
+dora_status check_desc(const dora_decode_desc* d);
+dora_status check_pack_desc(const dora_pack_desc* d);
+
 bool ws_layout(const dora_decode_desc& d, int64_t waves, WsLayout* out);
 
 struct DecodeParams {
@@ -176,6 +180,12 @@ dora_status decode_attn(const dora_decode_desc* desc, const void* q, const void*
                         const void* v_pages, const int32_t* block_table, const int32_t* seq_lens,
                         const int32_t* version_ids, void* out, void* workspace,
                         size_t workspace_bytes, hipStream_t s, hipEvent_t* ev);
+
+// DORA_FLAG_VALIDATE: range- and ownership-check every page id of the tables,
+// synchronously (err: one device int32 of scratch).
+dora_status validate_tables(const dora_decode_desc& d, const int32_t* block_table,
+                            const int32_t* seq_lens, const int32_t* version_ids, int32_t* err,
+                            hipStream_t s);
 
 struct ValidateParams {
   const int32_t* block_table;

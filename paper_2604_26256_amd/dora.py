@@ -93,6 +93,18 @@ _lib.dora_decode_attn_grouped.argtypes = [_DescP, _P, _P, _P, _P, _P, _P, _P, _I
 _lib.dora_decode_attn_grouped.restype = ctypes.c_int
 _lib.dora_kv_append.argtypes = [_DescP, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]
 _lib.dora_kv_append.restype = ctypes.c_int
+_lib.dora_decode_tree_workspace_bytes.argtypes = [_DescP, _I32]
+_lib.dora_decode_tree_workspace_bytes.restype = _SZ
+_lib.dora_decode_attn_tree.argtypes = [_DescP, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                       _SZ, _P]
+_lib.dora_decode_attn_tree.restype = ctypes.c_int
+_lib.dora_decode_window_workspace_bytes.argtypes = [_DescP, _I32, _I32]
+_lib.dora_decode_window_workspace_bytes.restype = _SZ
+_lib.dora_decode_attn_window.argtypes = [_DescP, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+_lib.dora_decode_attn_window.restype = ctypes.c_int
+_lib.dora_kv_append_path.argtypes = [_DescP, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                     _P]
+_lib.dora_kv_append_path.restype = ctypes.c_int
 _lib.dora_plan_partition.argtypes = [ctypes.POINTER(_I64), _I32, _I32, ctypes.POINTER(_I32)]
 _lib.dora_plan_partition.restype = ctypes.c_int
 _lib.dora_plan_supplement.argtypes = [ctypes.POINTER(_I32), ctypes.POINTER(_I32), _I32, _I32,
@@ -104,6 +116,8 @@ _lib.dora_kv_page_pack.argtypes = [_PackP, _P, _P, _P, _P, _P, _I64, _P, _SZ, _P
 _lib.dora_kv_page_pack.restype = ctypes.c_int
 _lib.dora_kv_page_unpack.argtypes = [_PackP, _I32, _P, _SZ, _P, _I64, _P, _P, _P, _P, _P, _P]
 _lib.dora_kv_page_unpack.restype = ctypes.c_int
+_lib.dora_kv_page_copy.argtypes = [_PackP, _P, _P, _P, _P, _P, _P, _I64, _P, _P]
+_lib.dora_kv_page_copy.restype = ctypes.c_int
 _lib.dora_pool_create.argtypes = [_I64, _I32, _I32, ctypes.c_uint64, ctypes.POINTER(_P)]
 _lib.dora_pool_create.restype = ctypes.c_int
 _lib.dora_pool_destroy.argtypes = [_P]
@@ -127,6 +141,13 @@ _lib.dora_pool_stats.restype = ctypes.c_int
 _lib.dora_pool_migrate_seq.argtypes = [_P, _I64, _P, _I32, ctypes.POINTER(_I64), _P, _P, _I32,
                                        ctypes.POINTER(_I32)]
 _lib.dora_pool_migrate_seq.restype = ctypes.c_int
+_lib.dora_pool_fork_seq.argtypes = [_P, _I64, _I32, ctypes.POINTER(_I64), ctypes.POINTER(_I32),
+                                    ctypes.POINTER(_I32), ctypes.POINTER(_I32)]
+_lib.dora_pool_fork_seq.restype = ctypes.c_int
+_lib.dora_pool_release_window.argtypes = [_P, _I64, _I32, _I32, ctypes.POINTER(_I32)]
+_lib.dora_pool_release_window.restype = ctypes.c_int
+_lib.dora_pool_compact.argtypes = [_P, _P, _P, _I32, ctypes.POINTER(_I32)]
+_lib.dora_pool_compact.restype = ctypes.c_int
 
 
 def library():
@@ -554,6 +575,228 @@ def dora_kv_append(k_new, v_new, block_table, seq_lens, k_pages, v_pages, *, num
            "dora_kv_append")
 
 
+def dora_decode_tree_workspace_bytes(desc: dora_decode_desc, num_nodes) -> int:
+    """Workspace of dora_decode_attn_tree (0 on invalid arguments)."""
+    return int(_lib.dora_decode_tree_workspace_bytes(ctypes.byref(desc), int(num_nodes)))
+
+
+def dora_decode_window_workspace_bytes(desc: dora_decode_desc, window, sinks) -> int:
+    """Workspace of dora_decode_attn_window (0 on invalid arguments)."""
+    return int(_lib.dora_decode_window_workspace_bytes(ctypes.byref(desc), int(window), int(sinks)))
+
+
+def _one_device(device, stream, *tensors):
+    """Raises unless every tensor given, and the stream, is on `device`."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and on {t.device}: one call works on one GPU")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"tensors on {device}, stream on {stream.device}")
+
+
+def _call(device, stream, fn, *args):
+    """fn(*args, stream handle) with `device` current (the library launches on the current one)."""
+    torch = _torch()
+    if torch.cuda.current_device() == device.index:
+        return fn(*args, _stream_handle(stream, device))
+    with torch.cuda.device(device):
+        return fn(*args, _stream_handle(stream, device))
+
+
+def _own_workspace(cache, device, stream, need):
+    """The cached workspace of (device, stream); while a graph is captured a new one, from the
+    graph's own memory, so that no two graphs share one."""
+    torch = _torch()
+    if torch.cuda.is_current_stream_capturing():
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
+            return torch.empty(need, dtype=torch.uint8, device=device)
+    return _cached_workspace(cache, device, stream, need)
+
+
+_tree_ws_cache = {}
+_window_ws_cache = {}
+
+
+def dora_decode_attn_tree(q, k_draft, v_draft, tree_mask, k_pages, v_pages, block_table, seq_lens,
+                          version_ids, out, *, num_kv_heads, page_size, kv_dtype=DORA_KV_BF16,
+                          sm_scale=0.0, k_scales=None, v_scales=None, page_owner=None, flags=0,
+                          num_waves=0, node_counts=None, workspace=None, stream=None):
+    """Decode attention of a tree of drafted tokens per sequence (see include/dora.h).
+
+    q, out: bf16 [B][T][Hq][d]; k_draft, v_draft: bf16 [B][T][Hkv][d]; tree_mask: int64 (or
+    uint64) [B][T], bit j of [b][i] set where node i attends node j; node_counts: optional
+    int32 [B], nodes of each sequence (rows behind them are left as they were); seq_lens:
+    the cached tokens, which every node attends.  Other arguments as for dora_decode_attn.
+    Returns `out`."""
+    torch = _torch()
+    if q.dim() != 4:
+        raise ValueError("q must be [B][num_nodes][num_q_heads][head_dim]")
+    B, T, Hq, D = (int(x) for x in q.shape)
+    num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B][stride]")
+    stride = int(block_table.shape[1])
+    fp8 = kv_dtype == DORA_KV_FP8_E4M3
+    desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
+                            page_size=page_size, block_table_stride=max(1, stride),
+                            num_pages=num_pages, kv_dtype=kv_dtype, sm_scale=sm_scale,
+                            k_scales=k_scales, v_scales=v_scales, page_owner=page_owner,
+                            flags=flags, num_waves=num_waves)
+    if B == 0:
+        return out
+    bf16, i32, drafts = (torch.bfloat16,), (torch.int32,), (B, T, num_kv_heads, D)
+    args = [
+        T,
+        _dev_ptr(q, "q", bf16),
+        _dev_ptr(k_draft, "k_draft", bf16, shape=drafts),
+        _dev_ptr(v_draft, "v_draft", bf16, shape=drafts),
+        _dev_ptr(tree_mask, "tree_mask", (torch.int64, torch.uint64), shape=(B, T), align=8),
+        _opt_ptr(node_counts, "node_counts", i32, shape=(B,), align=4),
+        _dev_ptr(k_pages, "k_pages", kv_types),
+        _dev_ptr(v_pages, "v_pages", kv_types),
+        _dev_ptr(block_table, "block_table", i32, shape=(B, stride), align=4),
+        _dev_ptr(seq_lens, "seq_lens", i32, shape=(B,), align=4),
+        _opt_ptr(version_ids, "version_ids", i32, shape=(B,), align=4),
+        _dev_ptr(out, "out", bf16, shape=(B, T, Hq, D)),
+    ]
+    if fp8:
+        _dev_ptr(k_scales, "k_scales", (torch.float32,), shape=(num_pages,), align=4)
+        _dev_ptr(v_scales, "v_scales", (torch.float32,), shape=(num_pages,), align=4)
+    if page_owner is not None:
+        _dev_ptr(page_owner, "page_owner", (torch.int16,), shape=(num_pages,), align=2)
+    _one_device(q.device, stream, k_draft, v_draft, tree_mask, node_counts, k_pages, v_pages,
+                block_table, seq_lens, version_ids, out, k_scales if fp8 else None,
+                v_scales if fp8 else None, page_owner, workspace)
+    need = _call_bytes(q.device, _lib.dora_decode_tree_workspace_bytes, desc, T)
+    if need == 0:  # invalid or unsupported: let the library name the reason
+        _check(_call(q.device, stream, _lib.dora_decode_attn_tree, ctypes.byref(desc), *args, None,
+                     0), "dora_decode_attn_tree")
+    if workspace is None:
+        workspace = _own_workspace(_tree_ws_cache, q.device, stream, need)
+    _check(_call(q.device, stream, _lib.dora_decode_attn_tree, ctypes.byref(desc), *args,
+                 _dev_ptr(workspace, "workspace", (torch.uint8,)), workspace.numel()),
+           "dora_decode_attn_tree")
+    return out
+
+
+def _call_bytes(device, fn, desc, *args):
+    """A workspace size with `device` current (it goes by the device's compute units)."""
+    torch = _torch()
+    if torch.cuda.current_device() == device.index:
+        return int(fn(ctypes.byref(desc), *args))
+    with torch.cuda.device(device):
+        return int(fn(ctypes.byref(desc), *args))
+
+
+def dora_decode_attn_window(q, k_pages, v_pages, block_table, seq_lens, version_ids, out, *,
+                            window, sinks=0, num_kv_heads, page_size, kv_dtype=DORA_KV_BF16,
+                            sm_scale=0.0, k_scales=None, v_scales=None, page_owner=None, flags=0,
+                            workspace=None, stream=None):
+    """Decode attention over the last `window` tokens of each sequence and its first `sinks`
+    (see include/dora.h); pages that hold neither are not read.  Other arguments as for
+    dora_decode_attn.  Returns `out`."""
+    desc, args = _decode_args(q, k_pages, v_pages, block_table, seq_lens, version_ids, out,
+                              num_kv_heads=num_kv_heads, page_size=page_size, kv_dtype=kv_dtype,
+                              sm_scale=sm_scale, k_scales=k_scales, v_scales=v_scales,
+                              page_owner=page_owner, flags=flags, num_waves=0, min_range_pages=0)
+    window, sinks = int(window), int(sinks)
+    if not -2**31 <= window < 2**31 or not -2**31 <= sinks < 2**31:
+        raise ValueError("window and sinks are 32-bit token counts")
+    if args is None:
+        return out
+    fp8 = kv_dtype == DORA_KV_FP8_E4M3
+    _one_device(q.device, stream, k_pages, v_pages, block_table, seq_lens, version_ids, out,
+                k_scales if fp8 else None, v_scales if fp8 else None, page_owner, workspace)
+    need = _call_bytes(q.device, _lib.dora_decode_window_workspace_bytes, desc, window, sinks)
+    if need == 0:  # invalid or unsupported: let the library name the reason
+        _check(_call(q.device, stream, _lib.dora_decode_attn_window, ctypes.byref(desc), window,
+                     sinks, *args, None, 0), "dora_decode_attn_window")
+    if workspace is None:
+        workspace = _own_workspace(_window_ws_cache, q.device, stream, need)
+    _check(_call(q.device, stream, _lib.dora_decode_attn_window, ctypes.byref(desc), window, sinks,
+                 *args, _dev_ptr(workspace, "workspace", (_torch().uint8,)), workspace.numel()),
+           "dora_decode_attn_window")
+    return out
+
+
+def dora_kv_append_path(k_new, v_new, block_table, seq_lens, k_pages, v_pages, *, num_kv_heads,
+                        page_size, path=None, counts=None, kv_dtype=DORA_KV_BF16, k_scales=None,
+                        v_scales=None, version_ids=None, page_owner=None, flags=0,
+                        dev_status=None, stream=None):
+    """Store several tokens of each sequence, in place (see include/dora.h): rows path[b][i]
+    (row i without path) of k_new / v_new (bf16 [B][T][Hkv][d]), i < counts[b] (T without
+    counts), become the last tokens of the seq_lens[b] that the sequence then has."""
+    torch = _torch()
+    if k_new.dim() != 4 or int(k_new.shape[2]) != num_kv_heads:
+        raise ValueError("k_new must be [B][T][num_kv_heads][head_dim]")
+    B, T, Hkv, D = (int(x) for x in k_new.shape)
+    num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B][stride]")
+    stride = int(block_table.shape[1])
+    desc = make_decode_desc(num_seqs=B, num_q_heads=num_kv_heads, num_kv_heads=num_kv_heads,
+                            head_dim=D, page_size=page_size, block_table_stride=max(1, stride),
+                            num_pages=num_pages, kv_dtype=kv_dtype, page_owner=page_owner,
+                            flags=flags)
+    if B == 0:
+        return
+    fp8 = kv_dtype == DORA_KV_FP8_E4M3
+    bf16, i32, f32 = (torch.bfloat16,), (torch.int32,), (torch.float32,)
+    args = [
+        T,
+        _dev_ptr(k_new, "k_new", bf16),
+        _dev_ptr(v_new, "v_new", bf16, shape=(B, T, Hkv, D)),
+        _opt_ptr(path, "path", i32, shape=(B, T), align=4),
+        _opt_ptr(counts, "counts", i32, shape=(B,), align=4),
+        _dev_ptr(block_table, "block_table", i32, shape=(B, stride), align=4),
+        _dev_ptr(seq_lens, "seq_lens", i32, shape=(B,), align=4),
+        _opt_ptr(version_ids, "version_ids", i32, shape=(B,), align=4),
+        _dev_ptr(k_pages, "k_pages", kv_types),
+        _dev_ptr(v_pages, "v_pages", kv_types),
+        _dev_ptr(k_scales, "k_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
+        _dev_ptr(v_scales, "v_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
+        _opt_ptr(dev_status, "dev_status", i32, numel=1, align=4),
+    ]
+    if page_owner is not None:
+        _dev_ptr(page_owner, "page_owner", (torch.int16,), shape=(num_pages,), align=2)
+    _one_device(k_new.device, stream, v_new, path, counts, block_table, seq_lens, version_ids,
+                k_pages, v_pages, k_scales if fp8 else None, v_scales if fp8 else None, dev_status,
+                page_owner)
+    _check(_call(k_new.device, stream, _lib.dora_kv_append_path, ctypes.byref(desc), *args),
+           "dora_kv_append_path")
+
+
+def dora_kv_page_copy(k_pages, v_pages, src_pages, dst_pages, *, num_kv_heads, page_size, head_dim,
+                      kv_dtype=DORA_KV_BF16, k_scales=None, v_scales=None, dev_status=None,
+                      stream=None):
+    """Copy pages src_pages of a pool to its pages dst_pages (device int32 lists of the same
+    length), K, V and fp8 scales (see include/dora.h)."""
+    torch = _torch()
+    num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, head_dim,
+                                       kv_dtype)
+    n = int(src_pages.numel())
+    if int(dst_pages.numel()) != n:
+        raise ValueError("src_pages and dst_pages must have the same length")
+    desc = make_pack_desc(kv_dtype=kv_dtype, page_size=page_size, num_kv_heads=num_kv_heads,
+                          head_dim=head_dim, num_pages=num_pages, policy_version=0)
+    fp8 = kv_dtype == DORA_KV_FP8_E4M3
+    i32, f32 = (torch.int32,), (torch.float32,)
+    args = [
+        _dev_ptr(k_pages, "k_pages", kv_types),
+        _dev_ptr(v_pages, "v_pages", kv_types),
+        _dev_ptr(k_scales, "k_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
+        _dev_ptr(v_scales, "v_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
+        _dev_ptr(src_pages, "src_pages", i32, align=4) if n else None,
+        _dev_ptr(dst_pages, "dst_pages", i32, align=4) if n else None,
+        n,
+        _opt_ptr(dev_status, "dev_status", i32, numel=1, align=4),
+    ]
+    _one_device(k_pages.device, stream, v_pages, src_pages if n else None, dst_pages if n else None,
+                k_scales if fp8 else None, v_scales if fp8 else None, dev_status)
+    _check(_call(k_pages.device, stream, _lib.dora_kv_page_copy, ctypes.byref(desc), *args),
+           "dora_kv_page_copy")
+
+
 def plan_partition(workload, n_groups):
     """DP groups per policy version (oldest first) in proportion to workload."""
     n = len(workload)
@@ -735,3 +978,32 @@ class Pool:
                                           dstp.ctypes.data_as(_P), cap, ctypes.byref(got)),
                "dora_pool_migrate_seq")
         return new_id.value, src[:got.value], dstp[:got.value]
+
+    def fork_seq(self, seq_id: int, num_tokens: Optional[int] = None):
+        """A new sequence with the first num_tokens tokens (default: all) of seq_id, sharing the
+        pages they fill.  Returns (new_seq_id, src_pages, dst_pages): at most one page to copy
+        with dora_kv_page_copy."""
+        if num_tokens is None:
+            num_tokens = self.seq_info(seq_id)[0]
+        new_id, src, dst, n = ctypes.c_int64(), ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
+        _check(_lib.dora_pool_fork_seq(self._h, seq_id, num_tokens, ctypes.byref(new_id),
+                                       ctypes.byref(src), ctypes.byref(dst), ctypes.byref(n)),
+               "dora_pool_fork_seq")
+        return (new_id.value, np.array([src.value], np.int32)[:n.value],
+                np.array([dst.value], np.int32)[:n.value])
+
+    def release_window(self, seq_id: int, window: int, sinks: int = 0) -> int:
+        """Release the pages of seq_id that no later window decode reads; how many it released."""
+        n = ctypes.c_int32()
+        _check(_lib.dora_pool_release_window(self._h, seq_id, window, sinks, ctypes.byref(n)),
+               "dora_pool_release_window")
+        return n.value
+
+    def compact(self):
+        """Move the live pages to the pool's start.  Returns (src_pages, dst_pages) to copy with
+        dora_kv_page_copy; block tables taken before are stale."""
+        src, dst = np.zeros(self.num_pages, np.int32), np.zeros(self.num_pages, np.int32)
+        n = ctypes.c_int32()
+        _check(_lib.dora_pool_compact(self._h, src.ctypes.data_as(_P), dst.ctypes.data_as(_P),
+                                      self.num_pages, ctypes.byref(n)), "dora_pool_compact")
+        return src[:n.value].copy(), dst[:n.value].copy()

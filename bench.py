@@ -80,7 +80,8 @@ COMPUTE_CMD = ("cd /tmp && timeout -s KILL 300 rocprofv3 --pmc {c} --output-form
 # Every kernel that a summary under profiles/ names, and the rules that launch them.
 KERNEL_SOURCES = [os.path.join(ROOT, "paper_2604_26256_amd", "csrc", f)
                   for f in ("decode.hip", "segment.hip", "grouped.hip", "append.hip", "pack.hip",
-                            "tree.hip", "window.hip", "append_path.hip", "page_copy.hip",
+                            "tree.hip", "tree_narrow.hip", "tree_core.h", "window.hip",
+                            "append_path.hip", "page_copy.hip",
                             "decode_core.h", "merge_core.h", "fp8_core.h", "dora_internal.h",
                             "cache_internal.h", "api.cpp")]
 

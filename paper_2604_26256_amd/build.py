@@ -22,8 +22,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdora.so")
 ARCH = "gfx950"
 
-HIP_SOURCES = ["tree.hip", "window.hip", "decode.hip", "segment.hip", "pack.hip", "append.hip",
-               "append_path.hip", "page_copy.hip", "grouped.hip", "measure.hip", "noalloc.hip"]
+HIP_SOURCES = ["tree.hip", "tree_narrow.hip", "window.hip", "decode.hip", "segment.hip", "pack.hip",
+               "append.hip", "append_path.hip", "page_copy.hip", "grouped.hip", "measure.hip", "noalloc.hip"]
 CXX_SOURCES = ["api.cpp", "cache_api.cpp", "pool.cpp", "plan.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]

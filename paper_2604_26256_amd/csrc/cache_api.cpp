@@ -42,7 +42,8 @@ dora_status check_attn(const dora_decode_desc& d, const void* q, const void* k_p
 
 float scale_log2_of(const dora_decode_desc& d) {
   const float scale = d.sm_scale > 0.f ? d.sm_scale : 1.0f / sqrtf((float)d.head_dim);
-  return scale * 1.4426950408889634f;
+  // (the kernels take it for positive)
+  return fmaxf(scale * 1.4426950408889634f, 1e-30f);
 }
 
 int64_t page_bytes_of(const dora_decode_desc& d) {
@@ -70,14 +71,12 @@ void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
   const int64_t columns = (int64_t)num_nodes * (d.num_q_heads / d.num_kv_heads);
   t->tiles = tree_tiles(columns);
   t->blocks = (int)((columns + 32 * t->tiles - 1) / (32 * t->tiles));
-  // A launch's stages are counted in 32 bits.
-  const int64_t steps = ((int64_t)d.block_table_stride * d.page_size + 31) / 32 + 2;
+  // A launch's stages (a segment's start counts as some) are counted in 32 bits.
+  const int64_t steps = ((int64_t)d.block_table_stride * d.page_size + 31) / 32 + 2 + 8;
   int64_t seqs = INT32_MAX / (steps * d.num_kv_heads * t->blocks);
   if (seqs > kTreeMaxSeqs) seqs = kTreeMaxSeqs;
   t->seqs = (int)(seqs < d.num_seqs ? seqs : d.num_seqs);
-  const int64_t slots =
-      (int64_t)compute_units() * tree_workgroups_per_cu(d.head_dim, d.page_size,
-                                                        d.kv_dtype == DORA_KV_FP8_E4M3, t->tiles);
+  const int64_t slots = (int64_t)compute_units() * (t->tiles <= 2 && d.head_dim == 128 && d.kv_dtype == DORA_KV_BF16 ? 1 : 2);
   const int64_t most = (int64_t)t->seqs * d.num_kv_heads * t->blocks * steps;
   t->workgroups = d.num_waves > 0 ? (d.num_waves + kTreeWaves - 1) / kTreeWaves
                   : slots < most ? slots : most;
@@ -224,8 +223,10 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
     p.scale_log2 = scale_log2_of(d);
     const int64_t grid =
         p.whole ? (int64_t)p.num_seqs * d.num_kv_heads * t.blocks : t.workgroups;
-    if (launch_tree(p, d.head_dim, d.page_size, fp8, t.tiles, grid, s) != hipSuccess)
-      return DORA_ERR_HIP;
+    const hipError_t e =
+        t.tiles <= 2 ? launch_tree_narrow(p, d.head_dim, d.page_size, fp8, t.tiles, grid, s)
+                     : launch_tree_wide(p, d.head_dim, d.page_size, fp8, grid, s);
+    if (e != hipSuccess) return DORA_ERR_HIP;
     if (!p.whole && launch_tree_combine(p, d.head_dim, t.tiles, grid, s) != hipSuccess)
       return DORA_ERR_HIP;
   }

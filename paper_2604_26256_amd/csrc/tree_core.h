@@ -1,0 +1,231 @@
+// Device code that the tree attention kernels share: a sequence's stages, the range of
+// a workgroup in the batch's list of them, and the step over 32 tokens.  Included by
+// HIP sources only.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cache_internal.h"
+#include "decode_core.h"
+
+namespace dora {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Smallest range of a workgroup, in stages.
+constexpr int kTreeMinRange = 2;
+
+// Stages of a sequence (steps of 32 tokens, steps_per_stage at a time): cache_stages over
+// its cached tokens, then those of its drafts.  blocks: column blocks that have columns.
+struct TreeSeq {
+  int L, nodes, pages, cache_steps, cache_stages, stages, blocks;
+};
+
+__device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b, int P, int steps_per_stage,
+                                            int columns_per_block) {
+  TreeSeq s;
+  s.nodes = p.node_counts ? p.node_counts[b] : p.num_nodes;
+  s.nodes = s.nodes < 0 ? 0 : s.nodes < p.num_nodes ? s.nodes : p.num_nodes;
+  const int64_t most = (int64_t)p.stride * P;
+  int L = p.seq_lens[b];
+  L = L < 0 ? 0 : L;
+  s.L = L < most ? L : (int)most;  // a contract violation stays in bounds
+  s.pages = (s.L + P - 1) / P;
+  s.cache_steps = (int)(((int64_t)s.L + 31) / 32);
+  s.cache_stages = (s.cache_steps + steps_per_stage - 1) / steps_per_stage;
+  const int draft_steps = (s.nodes + 31) / 32;
+  s.stages = s.cache_stages + (draft_steps + steps_per_stage - 1) / steps_per_stage;
+  s.blocks = (s.nodes * p.group + columns_per_block - 1) / columns_per_block;
+  return s;
+}
+
+// This workgroup's range [x0, x1) of the batch's `total` stages, cut for W workgroups, and
+// the sequence b that holds x0.  Each segment counts as COST stages more than it has, in
+// front of them, so that ranges of many short segments take no longer than others.  pre: LDS,
+// [num_seqs + 1], the stages (over heads and blocks) before each sequence.
+struct TreeRange {
+  int x0, x1, total, W, b;
+};
+
+template <int P, int SP, int CB, int COST>
+__device__ __forceinline__ TreeRange tree_range(const TreeParams& p, int* pre) {
+  __shared__ int s_wave[kTreeWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), B = p.num_seqs;
+  int carry = 0;
+  for (int base = 0; base < B; base += 64 * kTreeWaves) {
+    int n = 0;
+    if (base + tid < B) {
+      const TreeSeq s = tree_seq(p, base + tid, P, SP, CB);
+      n = s.blocks ? (s.stages + COST) * s.blocks * p.num_kv_heads : 0;
+    }
+    int incl = n;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(incl, off);
+      if (lane >= off) incl += y;
+    }
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    int before = carry;
+    for (int w = 0; w < kTreeWaves; ++w) {
+      if (w < wave) before += s_wave[w];
+      carry += s_wave[w];
+    }
+    if (base + tid < B) pre[base + tid] = before + incl - n;
+    __syncthreads();
+  }
+  if (tid == 0) pre[B] = carry;
+  __syncthreads();
+  TreeRange r;
+  r.total = uni(carry);
+  // Ranges of kTreeMinRange stages at least, none empty: the pieces of a cut segment are on
+  // neighbouring workgroups.
+  const int most = (r.total + kTreeMinRange - 1) / kTreeMinRange;
+  r.W = most < (int)gridDim.x ? most : (int)gridDim.x;
+  r.x0 = r.x1 = r.b = 0;
+  if ((int)blockIdx.x >= r.W) return r;
+  r.x0 = (int)((int64_t)r.total * blockIdx.x / r.W);
+  r.x1 = (int)((int64_t)r.total * (blockIdx.x + 1) / r.W);
+  int lo = 0, hi = B;  // the last sequence with pre <= x0
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (pre[mid] <= r.x0) lo = mid; else hi = mid;
+  }
+  r.b = uni(lo);
+  return r;
+}
+
+// Workgroups that hold pieces of a segment whose first piece is this workgroup's and whose
+// last stage is `last`.
+__device__ __forceinline__ int tree_pieces(const TreeRange& r, int last) {
+  int w = (int)((int64_t)last * r.W / r.total);  // near the range that holds `last`
+  while (w + 1 < r.W && (int64_t)r.total * (w + 1) / r.W <= last) ++w;
+  while ((int64_t)r.total * w / r.W > last) --w;
+  return w - (int)blockIdx.x + 1;
+}
+
+// What the 8 accumulator registers of a page's tokens are scaled by.  fp8: the page's V
+// scale goes into the exponent, so that the largest weight of a column is 1 and its
+// rounding to bf16 exact (a weight that is rounded after the scaling adds 0.0018 to a
+// peaked row's relative error of 0.0017, so it adds 0.0012); the sum of the weights is
+// over 2^add then.  A V scale that has no such logarithm (0, negative, not finite, far from
+// 1) stays a factor.
+struct TreeScale {
+  float mul;   // scores
+  float add;   // added to the scaled scores, log2 units
+  float inv;   // 2^-add
+  float left;  // what remains of the V scale: 1, or the scale itself
+};
+
+template <bool FP8>
+__device__ __forceinline__ TreeScale tree_scale(float scale_log2, float k_scale, float v_scale) {
+  if constexpr (!FP8) {
+    return TreeScale{scale_log2, 0.f, 1.f, 1.f};
+  } else {
+    const bool fine = v_scale > 0x1p-40f && v_scale < 0x1p40f;
+    const float add = fine ? __builtin_amdgcn_logf(v_scale) : 0.f;
+    return TreeScale{scale_log2 * k_scale, add, fine ? __builtin_amdgcn_rcpf(v_scale) : 1.f,
+                     fine ? 1.f : v_scale};
+  }
+}
+
+// A step over 32 tokens for a tile of 32 columns: S^T = K Q^T, online softmax in the log2
+// domain, O^T += V^T P^T.  Lane (column lane & 31, half h = lane >> 5) holds in its
+// registers 8s + e the scores of the 8 tokens that it supplies to k-step s of the second
+// product.  kf(ks): K operand of 16 head-dim values; vf(i, s): V operand of head-dim rows
+// 32i .. 32i + 31 and k-step s.  s0, s1: the scales of registers 0-7 and 8-15.  bits: the
+// registers that count for the lane's column, where some does not (masked, uniform: a
+// branch around the scores alone, as a second copy of the step would need registers for a
+// second set of accumulators).
+//   AHEAD: the operands come from LDS.  All of K's are read before the first product and
+// all of V's before the softmax, so that the reads' latency is waited for once, and the
+// second time behind the softmax (the compiler by itself reads two ahead).
+template <int D, bool FP8, bool AHEAD, typename KF, typename VF>
+__device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale s1, bool masked,
+                                          uint32_t bits, const bf16x8 (&qop)[D / 16],
+                                          f32x16 (&acc)[D / 32], float& m_run, float& l_run) {
+  constexpr int KS = D / 16, DB = D / 32;
+  f32x16 sc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+  bf16x8 op[AHEAD ? KS : 1];
+  if constexpr (AHEAD) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) op[ks] = kf(ks);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    if constexpr (AHEAD)
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[ks], qop[ks], sc, 0, 0, 0);
+    else
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf(ks), qop[ks], sc, 0, 0, 0);
+  }
+  if constexpr (AHEAD) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) op[k] = vf(k >> 1, k & 1);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (FP8 && !(s0.mul > 0.f && s1.mul > 0.f)) {  // uniform: the maximum below needs mul > 0
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] *= r < 8 ? s0.mul : s1.mul;
+    s0.mul = s1.mul = 1.f;
+  }
+  if (masked)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (!((bits >> r) & 1u)) sc[r] = -__builtin_inff();
+  float mx = sc[0], mx1 = sc[8];
+#pragma unroll
+  for (int r = 1; r < 8; ++r) {
+    mx = fmaxf(mx, sc[r]);
+    mx1 = fmaxf(mx1, sc[8 + r]);
+  }
+  if constexpr (FP8)
+    mx = fmaxf(__builtin_fmaf(mx, s0.mul, s0.add), __builtin_fmaf(mx1, s1.mul, s1.add));
+  else
+    mx = fmaxf(mx, mx1) * s0.mul;
+  mx = max_xor32(mx);
+  if (__ballot(mx > m_run)) {  // some column's maximum grows: rescale the tile
+    const float m_new = fmaxf(m_run, mx);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
+  }
+  const float b0 = FP8 ? s0.add - m_run : -m_run, b1 = FP8 ? s1.add - m_run : -m_run;
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    sc[r] = __builtin_amdgcn_exp2f(
+        __builtin_fmaf(sc[r], FP8 && r >= 8 ? s1.mul : s0.mul, r < 8 ? b0 : b1));
+    sum[r >> 3] += sc[r];
+  }
+  if constexpr (FP8) {
+    l_run = __builtin_fmaf(sum[0], s0.inv, __builtin_fmaf(sum[1], s1.inv, l_run));
+    if (s0.left != 1.f || s1.left != 1.f)  // uniform
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] *= r < 8 ? s0.left : s1.left;
+  } else {
+    l_run += sum[0] + sum[1];
+  }
+  bf16x8 pb[2];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) pb[r >> 3][r & 7] = (__bf16)sc[r];
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if constexpr (AHEAD)
+        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[2 * i + s], pb[s], acc[i], 0, 0, 0);
+      else
+        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf(i, s), pb[s], acc[i], 0, 0, 0);
+    }
+}
+
+}  // namespace dora

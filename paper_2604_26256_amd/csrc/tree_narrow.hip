@@ -1,0 +1,375 @@
+// Tree attention for few columns (nodes x group) per KV head: a tile of 32 columns per
+// wave, a team of as many waves as there are tiles, and the teams take a workgroup's
+// steps in turn.  A wave loads its steps straight from HBM into matrix operands; the
+// waves of a team read the same lines, which come out of the caches but for the first.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tree_core.h"
+
+namespace dora {
+
+// What a segment costs besides its stages (lengths, page ids, queries, the merge), in stages.
+constexpr int kTreeNarrowCost = 2;
+
+// Lane (row of K's tile or of V's, half h) and the 32 tokens of a step.  Register 8s + 4j +
+// i of a lane is row 16s + 8j + 4h + i of the scores' tile; so that its 8 registers of
+// k-step s are 8 consecutive tokens, row r holds token row_token(r).  Where a V row of a
+// page is 32 bytes (fp8, 32 tokens), the lane's 16 tokens are consecutive: one 16-byte load.
+template <int P, bool FP8>
+struct TreeTokens {
+  static constexpr bool RUN16 = FP8 && P == 32;
+  static __device__ __forceinline__ int of_row(int r) {  // bits s j h i1 i0
+    const int s = (r >> 4) & 1, j = (r >> 3) & 1, h = (r >> 2) & 1;
+    return (RUN16 ? 16 * h + 8 * s : 16 * s + 8 * h) + 4 * j + (r & 3);
+  }
+  // Registers of half h whose tokens are among `bits`.
+  static __device__ __forceinline__ uint32_t registers(uint32_t bits, int h) {
+    if (RUN16) return (bits >> (16 * h)) & 0xFFFFu;
+    return ((bits >> (8 * h)) & 0xFFu) | (((bits >> (16 + 8 * h)) & 0xFFu) << 8);
+  }
+};
+
+// A step's K and V as a lane loads them: K in 16-byte pieces, V in 16 (8: fp8, 16 tokens)
+// bytes per 32 head-dim rows and k-step (or both k-steps).
+template <int D, int P, bool FP8>
+struct TreeRegs {
+  static constexpr int NK = FP8 ? D / 32 : D / 16;
+  static constexpr bool RUN16 = TreeTokens<P, FP8>::RUN16;
+  static constexpr int NV = (D / 32) * (RUN16 ? 1 : 2);
+  typedef typename std::conditional<FP8 && !RUN16, u32x2, u32x4>::type vraw_t;
+  u32x4 k[NK];
+  vraw_t v[NV];
+};
+
+template <bool NT, typename T>
+__device__ __forceinline__ T tree_load(const uint8_t* at) {
+  return NT ? __builtin_nontemporal_load((const T*)at) : *(const T*)at;
+}
+
+template <int D, int P, bool FP8, int TEAM>
+__global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_narrow_kernel(TreeParams p) {
+  constexpr int SP = kTreeWaves / TEAM, PAIR = 32 / P, CB = 32 * TEAM;
+  constexpr int KS = D / 16, DB = D / 32, E = FP8 ? 1 : 2;
+  constexpr int TILE = P * D * E;  // bytes of one (page, KV head) tile
+  constexpr int QUADS = 4 * DB;    // accumulator quads of a tile
+  typedef TreeRegs<D, P, FP8> R;
+  typedef TreeTokens<P, FP8> Tok;
+  __shared__ __align__(16) f32x4 s_o[kTreeWaves][QUADS][64];  // merge; a wave's draft V before
+  __shared__ float2 s_ml[kTreeWaves][32];
+  extern __shared__ int s_pre[];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+  const int col = lane & 31, h = lane >> 5;
+  const int team = wave / TEAM, tile = wave % TEAM;
+  const int Hkv = p.num_kv_heads, G = p.group;
+
+  TreeRange rg{0, 0, 0, 1, 0};
+  int b;
+  if (p.whole) {
+    b = (int)blockIdx.x / Hkv;
+  } else {
+    rg = tree_range<P, SP, CB, kTreeNarrowCost>(p, s_pre);
+    if (tid == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (rg.x0 >= rg.x1) return;  // uniform
+    b = rg.b;
+  }
+
+  // Per-lane byte offsets inside a (page, KV head) tile, and which of a step's two pages
+  // the lane's K token is on.
+  const int ktok = Tok::of_row(col);
+  const uint32_t koff = (uint32_t)((h * P + (ktok & (P - 1))) * 16);
+  const bool ksecond = PAIR == 2 && ktok >= 16;
+  const uint32_t voff = (uint32_t)(col * P * E + (Tok::RUN16 ? 16 * h : 8 * h * E));
+
+  bool first_piece = true;
+  int x = rg.x0;
+  while (true) {
+    // the piece: stages a .. z - 1 of (b, g)
+    const TreeSeq sq = tree_seq(p, b, P, SP, CB);
+    int g, a, z, taken = 0;
+    if (p.whole) {
+      g = (int)blockIdx.x - b * Hkv;
+      a = 0;
+      z = sq.stages;
+      if (sq.nodes == 0) return;  // uniform
+    } else {
+      const int r = x - s_pre[b], len = sq.stages + kTreeNarrowCost;
+      g = r / len;
+      a = r - g * len;
+      z = len - a < rg.x1 - x ? len : a + (rg.x1 - x);
+      taken = z - a;
+      a = a > kTreeNarrowCost ? a - kTreeNarrowCost : 0;
+      z -= kTreeNarrowCost;
+    }
+    if (z <= a) {  // uniform: nothing but a start, which is the next workgroup's
+      x += taken;
+      if (x >= rg.x1) return;
+      continue;
+    }
+    g = uni(g);
+    a = uni(a);
+    z = uni(z);
+    const int L = uni(sq.L), nodes = uni(sq.nodes), n_pages = uni(sq.pages);
+    const int cache_steps = uni(sq.cache_steps), cache_stages = uni(sq.cache_stages);
+
+    // this team's steps of the cache: st0, st0 + SP, ...; lane u holds the pages of its u-th
+    const int st0 = a * SP + team;
+    const int c_end = z < cache_stages ? z * SP : cache_steps;  // past the piece's last step
+    int steps = c_end > st0 ? (c_end - st0 + SP - 1) / SP : 0;
+    const int32_t* row_ids = p.block_table + (int64_t)b * p.stride;
+    int pid0 = 0, pid1 = 0;
+    auto load_ids = [&](int u0) {  // of the wave's steps u0 .. u0 + 63
+      const int j = (st0 + SP * (u0 + lane)) * PAIR;
+      const int last = n_pages - 1;
+      pid0 = row_ids[j < last ? j : last];
+      if constexpr (PAIR == 2) pid1 = row_ids[j + 1 < last ? j + 1 : last];
+    };
+    if (steps > 0) load_ids(0);
+
+    // query operand and mask: this lane's column.  fp8: a lane's 16-byte K piece is 16 head-dim
+    // values, its k-steps 2m and 2m + 1.
+    const int c = 32 * tile + col, node = c / G, head = c - node * G;
+    const bool mine = node < nodes;
+    const int64_t row = (((int64_t)b * p.num_nodes + (mine ? node : 0)) * p.num_q_heads +
+                         (int64_t)g * G + (mine ? head : 0));
+    bf16x8 qop[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      qop[s] = *(const bf16x8*)(p.q + row * D +
+                                (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
+    uint64_t sees = p.tree_mask[(int64_t)b * p.num_nodes + (mine ? node : 0)];
+    sees &= nodes >= 64 ? ~0ull : (1ull << nodes) - 1;
+    if (!mine) {
+      sees = 0;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qop[s] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    if (32 * tile >= nodes * G) steps = 0;  // uniform: the wave's tile has no columns
+
+    f32x16 acc[DB];
+    float m_run = kNoMax, l_run = 0.f;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+
+    // Cached tokens, 64 steps of the wave at a time (as many as lanes hold pages of).
+    for (int u0 = 0; u0 < steps; u0 += 64) {
+      if (u0 > 0) load_ids(u0);
+      const int n = steps - u0 < 64 ? steps - u0 : 64;
+      R buf[2];
+      float ks0[2], ks1[2], vs0[2], vs1[2];
+      auto prefetch = [&](int r, int u) {
+        const bool past = u >= n;  // past the last step the loads still issue, one line each
+        u = past ? n - 1 : u;
+        const int p0 = __builtin_amdgcn_readlane(pid0, u);
+        const int p1 = PAIR == 2 ? __builtin_amdgcn_readlane(pid1, u) : p0;
+        if constexpr (FP8) {
+          ks0[r] = p.k_scales[p0];
+          vs0[r] = p.v_scales[p0];
+          ks1[r] = PAIR == 2 ? p.k_scales[p1] : ks0[r];
+          vs1[r] = PAIR == 2 ? p.v_scales[p1] : vs0[r];
+        }
+        const int64_t base0 = (int64_t)p0 * p.page_bytes + (int64_t)g * TILE;
+        const int64_t base1 = (int64_t)p1 * p.page_bytes + (int64_t)g * TILE;
+        const uint8_t* kb = p.k_pages + (ksecond ? base1 : base0) + (past ? 0u : koff);
+#pragma unroll
+        for (int s = 0; s < R::NK; ++s)
+          buf[r].k[s] = tree_load<TEAM == 1, u32x4>(kb + s * (2 * P * 16));
+        const uint8_t* vb0 = p.v_pages + base0 + (past ? 0u : voff);
+        const uint8_t* vb1 = p.v_pages + base1 + (past ? 0u : voff);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+          typedef typename R::vraw_t V;
+          constexpr int BLK = 32 * P * E;  // bytes between 32-row blocks
+          if constexpr (R::RUN16) {
+            buf[r].v[i] = tree_load<TEAM == 1, V>(vb0 + i * BLK);
+          } else if constexpr (PAIR == 2) {
+            buf[r].v[2 * i] = tree_load<TEAM == 1, V>(vb0 + i * BLK);
+            buf[r].v[2 * i + 1] = tree_load<TEAM == 1, V>(vb1 + i * BLK);
+          } else {
+            buf[r].v[2 * i] = tree_load<TEAM == 1, V>(vb0 + i * BLK);
+            buf[r].v[2 * i + 1] = tree_load<TEAM == 1, V>(vb0 + i * BLK + 16 * E);
+          }
+        }
+      };
+      auto consume = [&](R& r, int u, float k0, float k1, float v0, float v1) {
+        const TreeScale s0 = tree_scale<FP8>(p.scale_log2, k0, v0);
+        const TreeScale s1 = PAIR == 2 ? tree_scale<FP8>(p.scale_log2, k1, v1) : s0;
+        const int nv = L - (st0 + SP * (u0 + u)) * 32;
+        const bool masked = nv < 32;
+        uint32_t own = 0xFFFFu;
+        if (masked) {  // slots past the sequence hold anything
+          own = Tok::registers((1u << nv) - 1u, h);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            u32x4 keep;  // of the 8 tokens of k-step s: bf16 words, or (first two) fp8 words
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              keep[w] = 0;
+#pragma unroll
+              for (int e = 0; e < (FP8 ? 4 : 2); ++e) {
+                constexpr int BITS = FP8 ? 8 : 16;
+                const int tok = 8 * s + (FP8 ? 4 : 2) * w + e;
+                if ((!FP8 || w < 2) && ((own >> tok) & 1u)) keep[w] |= ((1u << BITS) - 1u) << (BITS * e);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+              if constexpr (R::RUN16) {
+                r.v[i][2 * s] &= keep[0];
+                r.v[i][2 * s + 1] &= keep[1];
+              } else if constexpr (FP8) {
+                r.v[2 * i + s] &= u32x2{keep[0], keep[1]};
+              } else {
+                r.v[2 * i + s] &= keep;
+              }
+            }
+          }
+        }
+        auto kf = [&](int ks) -> bf16x8 {
+          if constexpr (FP8) {
+            const u32x4& w = r.k[ks >> 1];
+            return (ks & 1) ? fp8x8_to_bf16(w[2], w[3]) : fp8x8_to_bf16(w[0], w[1]);
+          } else {
+            return __builtin_bit_cast(bf16x8, r.k[ks]);
+          }
+        };
+        auto vf = [&](int i, int s) -> bf16x8 {
+          if constexpr (R::RUN16) {
+            return s ? fp8x8_to_bf16(r.v[i][2], r.v[i][3]) : fp8x8_to_bf16(r.v[i][0], r.v[i][1]);
+          } else if constexpr (FP8) {
+            return fp8x8_to_bf16(r.v[2 * i + s][0], r.v[2 * i + s][1]);
+          } else {
+            return __builtin_bit_cast(bf16x8, r.v[2 * i + s]);
+          }
+        };
+        tree_step<D, FP8, false>(kf, vf, s0, s1, masked, own, qop, acc, m_run, l_run);
+      };
+      // The page ids are waited for here, once.
+      asm volatile("" : "+v"(pid0), "+v"(pid1));
+      prefetch(0, 0);
+      for (int u = 0; u < n; u += 2) {
+        prefetch(1, u + 1);
+        consume(buf[0], u, ks0[0], ks1[0], vs0[0], vs1[0]);
+        // (no way out here: the compiler would wait at the top for what is loaded below)
+        prefetch(0, u + 2);
+        if (u + 1 < n) consume(buf[1], u + 1, ks0[1], ks1[1], vs0[1], vs1[1]);
+      }
+    }
+
+    // Drafts (the last stages).  V is turned round through the wave's part of LDS.
+    for (int st = a > cache_stages ? a : cache_stages; st < z; ++st) {
+      // the team with the fewest cache steps first
+      const int t0 = ((st - cache_stages) * SP + SP - 1 - team) * 32;
+      if (t0 >= nodes || 32 * tile >= nodes * G) continue;  // uniform in the wave
+      uint8_t* vt = (uint8_t*)&s_o[wave][0][0];  // [d][32 nodes], pieces of 8 displaced by row
+      auto v_at = [](int row_, int piece) { return row_ * 64 + ((piece ^ ((row_ >> 2) & 3)) << 4); };
+      for (int e = lane; e < 32 * (D / 8); e += 64) {
+        const int t = e / (D / 8), ch = e - t * (D / 8);
+        u32x4 vx{0u, 0u, 0u, 0u};
+        if (t0 + t < nodes)
+          vx = *(const u32x4*)(p.v_draft +
+                               (((int64_t)b * p.num_nodes + t0 + t) * Hkv + g) * D + 8 * ch);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          *(uint16_t*)(vt + v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
+              (uint16_t)(vx[i >> 1] >> (16 * (i & 1)));
+      }
+      const int t = t0 + ktok < nodes ? t0 + ktok : nodes - 1;  // a row past the nodes is masked
+      const uint16_t* kd = p.k_draft + (((int64_t)b * p.num_nodes + t) * Hkv + g) * D;
+      auto kf = [&](int s) -> bf16x8 {
+        return *(const bf16x8*)(kd + (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
+      };
+      auto vf = [&](int i, int s) -> bf16x8 {
+        return *(const bf16x8*)(vt + v_at(32 * i + col, Tok::RUN16 ? 2 * h + s : 2 * s + h));
+      };
+      const TreeScale one{p.scale_log2, 0.f, 1.f, 1.f};
+      tree_step<D, FP8, false>(kf, vf, one, one, true, Tok::registers((uint32_t)(sees >> t0), h), qop, acc,
+                        m_run, l_run);
+    }
+
+    // The piece's result: a tile's SP waves merged in LDS, each summing a share of the quads;
+    // then the rows, or one partial.
+    const bool whole = a == 0 && z == sq.stages;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (first_piece ? 0 : 1);
+    float S = sum_xor32(l_run), M = m_run;
+    if constexpr (SP > 1) {
+      if (h == 0) s_ml[wave][col] = make_float2(m_run, S);
+      __syncthreads();  // and every wave has done with its drafts
+#pragma unroll
+      for (int w = 0; w < SP; ++w) M = fmaxf(M, s_ml[w * TEAM + tile][col].x);
+      S = 0.f;
+#pragma unroll
+      for (int w = 0; w < SP; ++w) {
+        const float2 ml = s_ml[w * TEAM + tile][col];
+        S += ml.y * (ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M));
+      }
+      const float f = m_run == M ? 1.f : __builtin_amdgcn_exp2f(m_run - M);
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          s_o[wave][4 * i + j][lane] = f32x4{acc[i][4 * j] * f, acc[i][4 * j + 1] * f,
+                                             acc[i][4 * j + 2] * f, acc[i][4 * j + 3] * f};
+      __syncthreads();
+    }
+    const bool none = L == 0 && sees == 0;  // nothing to attend: zeros
+    const float inv = none ? 0.f : 1.f / S;
+#pragma unroll
+    for (int k = 0; k < QUADS / SP; ++k) {
+      const int quad = team + SP * k, i = quad >> 2, j = quad & 3;
+      f32x4 o;
+      if constexpr (SP > 1) {
+        o = s_o[tile][quad][lane];
+#pragma unroll
+        for (int w = 1; w < SP; ++w) o += s_o[w * TEAM + tile][quad][lane];
+      } else {
+        o = f32x4{acc[k >> 2][4 * (k & 3)], acc[k >> 2][4 * (k & 3) + 1], acc[k >> 2][4 * (k & 3) + 2],
+                  acc[k >> 2][4 * (k & 3) + 3]};
+      }
+      if (!whole)
+        ((f32x4*)(p.part_o + (slot * TEAM + tile) * 32 * D))[quad * 64 + lane] = o;
+      else if (mine)
+        *(bf16x4*)(p.out + row * D + 32 * i + 8 * j + 4 * h) =
+            bf16x4{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv),
+                   (__bf16)(o[3] * inv)};
+    }
+    if (!whole && team == 0 && h == 0)
+      p.part_ml[(slot * TEAM + tile) * 32 + col] = make_float2(M, S);
+    if (!whole && a == 0 && tid == 0)
+      p.cuts[blockIdx.x] = make_int4(b, g, tree_pieces(rg, x + taken + (sq.stages - z) - 1), (int)slot);
+    if (p.whole) return;
+    x += taken;
+    if (x >= rg.x1) return;  // uniform
+    first_piece = false;
+    while (s_pre[b + 1] <= x) ++b;
+    b = uni(b);
+    if constexpr (SP > 1) __syncthreads();  // s_o and s_ml: before the next piece's
+  }
+}
+
+template <int D, int P, bool FP8>
+static const void* narrow_fn(int tiles) {
+  return tiles == 1   ? (const void*)&tree_narrow_kernel<D, P, FP8, 1>
+         : tiles == 2 ? (const void*)&tree_narrow_kernel<D, P, FP8, 2>
+                      : (const void*)&tree_narrow_kernel<D, P, FP8, 4>;
+}
+
+hipError_t launch_tree_narrow(const TreeParams& p, int D, int P, bool fp8, int tiles, int64_t grid,
+                              hipStream_t s) {
+  const void* fn;
+  if (D == 128)
+    fn = P == 16 ? (fp8 ? narrow_fn<128, 16, true>(tiles) : narrow_fn<128, 16, false>(tiles))
+                 : (fp8 ? narrow_fn<128, 32, true>(tiles) : narrow_fn<128, 32, false>(tiles));
+  else
+    fn = P == 16 ? (fp8 ? narrow_fn<64, 16, true>(tiles) : narrow_fn<64, 16, false>(tiles))
+                 : (fp8 ? narrow_fn<64, 32, true>(tiles) : narrow_fn<64, 32, false>(tiles));
+  TreeParams arg = p;
+  void* args[] = {(void*)&arg};
+  const unsigned lds = p.whole ? 0 : (unsigned)(p.num_seqs + 1) * 4;
+  return hipLaunchKernel(fn, dim3((unsigned)grid), dim3(64 * kTreeWaves), args, lds, s);
+}
+
+}  // namespace dora

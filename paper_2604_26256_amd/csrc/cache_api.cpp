@@ -76,7 +76,7 @@ void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
   int64_t seqs = INT32_MAX / (steps * d.num_kv_heads * t->blocks);
   if (seqs > kTreeMaxSeqs) seqs = kTreeMaxSeqs;
   t->seqs = (int)(seqs < d.num_seqs ? seqs : d.num_seqs);
-  const int64_t slots = (int64_t)compute_units() * (t->tiles <= 2 && d.head_dim == 128 && d.kv_dtype == DORA_KV_BF16 ? 1 : 2);
+  const int64_t slots = (int64_t)compute_units() * (t->tiles < 2 && d.head_dim == 128 && d.kv_dtype == DORA_KV_BF16 ? 1 : 2);
   const int64_t most = (int64_t)t->seqs * d.num_kv_heads * t->blocks * steps;
   t->workgroups = d.num_waves > 0 ? (d.num_waves + kTreeWaves - 1) / kTreeWaves
                   : slots < most ? slots : most;
@@ -224,8 +224,8 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
     const int64_t grid =
         p.whole ? (int64_t)p.num_seqs * d.num_kv_heads * t.blocks : t.workgroups;
     const hipError_t e =
-        t.tiles <= 2 ? launch_tree_narrow(p, d.head_dim, d.page_size, fp8, t.tiles, grid, s)
-                     : launch_tree_wide(p, d.head_dim, d.page_size, fp8, grid, s);
+        t.tiles < 2 ? launch_tree_narrow(p, d.head_dim, d.page_size, fp8, t.tiles, grid, s)
+                     : launch_tree_wide(p, d.head_dim, d.page_size, fp8, t.tiles, grid, s);
     if (e != hipSuccess) return DORA_ERR_HIP;
     if (!p.whole && launch_tree_combine(p, d.head_dim, t.tiles, grid, s) != hipSuccess)
       return DORA_ERR_HIP;

@@ -11,7 +11,7 @@
 
 namespace dora {
 
-constexpr int kTreeTiles = kTreeWaves;  // of a column block
+constexpr int kTreeTiles = kTreeWaves;  // of a column block, at most
 // Pages whose ids (and fp8 scales) a workgroup holds in LDS at a time.
 constexpr int kTreeWindow = 512;
 // What a segment costs besides its steps (lengths, page ids, queries, the rows), in steps.
@@ -40,22 +40,25 @@ __device__ __forceinline__ int tree_v_at(int row, int piece) {
 // (sequence, KV head, column block).
 //   A step's pages go HBM -> registers (two steps in flight) -> LDS, fp8 widened to bf16 on
 // the way, so that the four waves share one read and one conversion.
-template <int D, int P, bool FP8>
+template <int D, int P, bool FP8, int NT>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) {
-  constexpr int TT = 64 * kTreeWaves, PAIR = 32 / P, NT = kTreeTiles;
+  constexpr int SP = kTreeWaves / NT, TT = 64 * NT, PAIR = 32 / P;
   constexpr int KS = D / 16, DB = D / 32, CB = 32 * NT;
+  constexpr int DEPTH = NT == 2 ? 1 : 2;
   constexpr int TILE = P * D * (FP8 ? 1 : 2);      // bytes of one (page, KV head) tile
   constexpr int NK = 32 * D * (FP8 ? 1 : 2) / 16;  // 16-byte pieces of a step's K (V: as many)
   constexpr int PER = 2 * NK / TT;                 // pieces of a thread
   constexpr int KB = 32 * D * 2;                   // LDS bytes of a step's K (V: as many)
   static_assert(2 * NK % TT == 0 && NK / PAIR % 64 == 0, "a wave's 64 pieces are on one page");
-  __shared__ __align__(16) uint8_t s_kv[2][2 * KB];
+  __shared__ __align__(16) uint8_t s_kv[2][SP][2 * KB];
   __shared__ int s_pid[kTreeWindow];
   __shared__ float s_ksc[FP8 ? kTreeWindow : 1], s_vsc[FP8 ? kTreeWindow : 1];
+  __shared__ float2 s_ml[kTreeWaves][32];
   extern __shared__ int s_pre[];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
+  const int team = wave / NT, tile = wave % NT, tt = tid - team * TT;
   const int Hkv = p.num_kv_heads, G = p.group;
 
   TreeRange rg{0, 0, 0, 1, 0};
@@ -63,7 +66,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
   if (p.whole) {
     b = (int)blockIdx.x / (Hkv * p.blocks);
   } else {
-    rg = tree_range<P, 1, CB, kTreeWideCost>(p, s_pre);
+    rg = tree_range<P, SP, CB, kTreeWideCost>(p, s_pre);
     if (tid == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if (rg.x0 >= rg.x1) return;  // uniform
     b = rg.b;
@@ -72,8 +75,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
   bool first_piece = true;
   int x = rg.x0;
   while (true) {
-    // the piece: steps a .. z - 1 of (b, g, block)
-    const TreeSeq sq = tree_seq(p, b, P, 1, CB);
+    // the piece: stages a .. z - 1 of (b, g, block)
+    const TreeSeq sq = tree_seq(p, b, P, SP, CB);
     int g, blk, a, z, taken = 0;
     if (p.whole) {
       const int r = (int)blockIdx.x - b * Hkv * p.blocks;
@@ -103,10 +106,10 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
     a = uni(a);
     z = uni(z);
     const int n_pages = uni(sq.pages), L = uni(sq.L), nodes = uni(sq.nodes);
-    const int cache_steps = uni(sq.cache_steps);
+    const int cache_steps = uni(sq.cache_steps), cache_stages = uni(sq.cache_stages);
 
     // query operand: this lane's column
-    const int c = blk * CB + wave * 32 + col;
+    const int c = blk * CB + tile * 32 + col;
     const int node = c / G, head = c - node * G;
     const bool mine = node < nodes;
     const int64_t row = (((int64_t)b * p.num_nodes + (mine ? node : 0)) * p.num_q_heads +
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
     }
     const uint64_t live = nodes >= 64 ? ~0ull : (1ull << nodes) - 1;
     const uint64_t sees = mine ? p.tree_mask[(int64_t)b * p.num_nodes + node] & live : 0ull;
-    const bool active = uni(blk * CB + wave * 32 < nodes * G);  // the wave's tile has columns
+    const bool active = uni(blk * CB + tile * 32 < nodes * G);  // the wave's tile has columns
 
     f32x16 acc[DB];
 #pragma unroll
@@ -130,23 +133,23 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
 
     // The step in buffer `buf`; masked: the tokens of `bits` alone count.
     auto consume = [&](int buf, bool masked, uint32_t bits, const TreeScale& s0, const TreeScale& s1) {
-      const uint8_t* kv = s_kv[buf];
+      const uint8_t* kv = s_kv[buf][team];
       const uint32_t own = masked ? tree_registers(bits, h) : 0xFFFFu;
-      tree_step<D, FP8, true>(
+      tree_step<D, FP8, NT == 4>(
           [&](int s) { return *(const bf16x8*)(kv + ((2 * s + h) * 32 + col) * 16); },
           [&](int i, int s) { return *(const bf16x8*)(kv + KB + tree_v_at(32 * i + col, 2 * s + h)); },
           s0, s1, masked, own, qop, acc, m_run, l_run);
     };
 
     // Cached tokens, in windows of the pages whose ids fit the LDS array.
-    constexpr int WST = kTreeWindow / PAIR;  // steps of a window
-    const int c_end = z < cache_steps ? z : cache_steps;
+    constexpr int WST = kTreeWindow / (PAIR * SP);  // stages of a window
+    const int c_end = z < cache_stages ? z : cache_stages;
     for (int w0 = a; w0 < c_end; w0 += WST) {
       const int n_st = c_end - w0 < WST ? c_end - w0 : WST;
-      const int j0 = w0 * PAIR;
+      const int j0 = w0 * SP * PAIR;
       const int n_win = n_pages - j0 < kTreeWindow ? n_pages - j0 : kTreeWindow;
       __syncthreads();  // the arrays and the buffers are free
-      for (int t = tid; t < n_win; t += TT) {
+      for (int t = tid; t < n_win; t += 64 * kTreeWaves) {
         const int pid = p.block_table[(int64_t)b * p.stride + j0 + t];
         s_pid[t] = pid;
         if constexpr (FP8) {
@@ -155,9 +158,9 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
         }
       }
       __syncthreads();
-      // Pages of step w0 + u (past the end the window's last).
+      // Pages of the team's step of stage w0 + u (past the end the window's last).
       auto page = [&](int u, int pg) {
-        const int at = u * PAIR + pg;
+        const int at = (u * SP + team) * PAIR + pg;
         return s_pid[at < n_win ? at : n_win - 1];
       };
       auto load = [&](u32x4 (&r)[PER], int u, int v0, int v1) {
@@ -167,7 +170,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
         const int64_t base1 = (int64_t)p1 * p.page_bytes + (int64_t)g * TILE;
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-          const int e0 = 64 * wave + TT * k;  // the wave's first piece
+          const int e0 = 64 * tile + TT * k;  // the wave's first piece
           const bool is_v = NK % TT == 0 ? TT * k >= NK : e0 >= NK;
           const int i0 = is_v ? e0 - NK : e0;
           const bool second = PAIR == 2 && i0 >= NK / 2;
@@ -177,12 +180,12 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
         }
       };
       auto store = [&](const u32x4 (&r)[PER], int u, int buf) {
-        uint8_t* kv = s_kv[buf];
-        const int nv = L - (w0 + u) * 32;  // tokens of the step that count
+        uint8_t* kv = s_kv[buf][team];
+        const int nv = L - ((w0 + u) * SP + team) * 32;  // tokens of the step that count
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-          const int e = tid + k * TT;
-          const bool is_v = NK % TT == 0 ? TT * k >= NK : 64 * wave + TT * k >= NK;
+          const int e = tt + k * TT;
+          const bool is_v = NK % TT == 0 ? TT * k >= NK : 64 * tile + TT * k >= NK;
           const int idx = is_v ? e - NK : e;
           const int pg = PAIR == 2 ? idx / (NK / 2) : 0, rem = PAIR == 2 ? idx - pg * (NK / 2) : idx;
           u32x4 w = r[k];
@@ -218,11 +221,12 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
         }
       };
       auto compute = [&](int u, int buf) {
-        if (!active || u >= n_st) return;  // uniform in the wave
-        const int nv = L - (w0 + u) * 32;
+        const int step = (w0 + u) * SP + team;
+        if (!active || u >= n_st || step >= cache_steps) return;  // uniform in the wave
+        const int nv = L - step * 32;
         float ks0 = 1.f, ks1 = 1.f, vs0 = 1.f, vs1 = 1.f;
         if constexpr (FP8) {
-          const int at = u * PAIR, at1 = PAIR == 2 && at + 1 < n_win ? at + 1 : at;
+          const int at = (u * SP + team) * PAIR, at1 = PAIR == 2 && at + 1 < n_win ? at + 1 : at;
           ks0 = s_ksc[at];
           vs0 = s_vsc[at];
           ks1 = s_ksc[at1];
@@ -232,39 +236,55 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
         const TreeScale s1 = PAIR == 2 ? tree_scale<FP8>(p.scale_log2, ks1, vs1) : s0;
         consume(buf, nv < 32, nv < 32 ? (1u << nv) - 1u : ~0u, s0, s1);
       };
-      // Two steps in flight in registers, two in LDS: step u + 1 goes from registers to LDS,
-      // and the loads of step u + 3 are issued, before step u is computed.
-      u32x4 r0[PER], r1[PER];
-      int v0 = page(1, 0), v1 = page(1, 1);
-      load(r0, 0, page(0, 0), page(0, 1));
-      load(r1, 1, v0, v1);
-      v0 = page(2, 0);
-      v1 = page(2, 1);
-      store(r0, 0, 0);
-      load(r0, 2, v0, v1);
-      for (int u = 0; u < n_st; u += 2) {
-        __syncthreads();
-        v0 = page(u + 3, 0);
-        v1 = page(u + 3, 1);
-        store(r1, u + 1, 1);
-        load(r1, u + 3, v0, v1);
-        compute(u, 0);
-        // (no way out here: the compiler would wait at the top for what is loaded below)
-        __syncthreads();
-        v0 = page(u + 4, 0);
-        v1 = page(u + 4, 1);
-        store(r0, u + 2, 0);
-        load(r0, u + 4, v0, v1);
-        compute(u + 1, 1);
+      if constexpr (DEPTH == 1) {
+        // One stage in flight in registers, two in LDS: stage u + 1 goes from registers to
+        // LDS, and the loads of stage u + 2 are issued, before stage u is computed.
+        u32x4 r0[PER];
+        load(r0, 0, page(0, 0), page(0, 1));
+        int v0 = page(1, 0), v1 = page(1, 1);
+        store(r0, 0, 0);
+        load(r0, 1, v0, v1);
+        for (int u = 0; u < n_st; ++u) {
+          __syncthreads();
+          v0 = page(u + 2, 0);
+          v1 = page(u + 2, 1);
+          store(r0, u + 1, (u + 1) & 1);
+          load(r0, u + 2, v0, v1);
+          compute(u, u & 1);
+        }
+      } else {
+        u32x4 r0[PER], r1[PER];
+        int v0 = page(1, 0), v1 = page(1, 1);
+        load(r0, 0, page(0, 0), page(0, 1));
+        load(r1, 1, v0, v1);
+        v0 = page(2, 0);
+        v1 = page(2, 1);
+        store(r0, 0, 0);
+        load(r0, 2, v0, v1);
+        for (int u = 0; u < n_st; u += 2) {
+          __syncthreads();
+          v0 = page(u + 3, 0);
+          v1 = page(u + 3, 1);
+          store(r1, u + 1, 1);
+          load(r1, u + 3, v0, v1);
+          compute(u, 0);
+          // (no way out here: the compiler would wait at the top for what is loaded below)
+          __syncthreads();
+          v0 = page(u + 4, 0);
+          v1 = page(u + 4, 1);
+          store(r0, u + 2, 0);
+          load(r0, u + 4, v0, v1);
+          compute(u + 1, 1);
+        }
       }
     }
 
     // Drafts: rows of [node][d], V turned round on the way into LDS.
-    for (int st = a > cache_steps ? a : cache_steps; st < z; ++st) {
-      const int t0 = (st - cache_steps) * 32;  // first node of the step
+    for (int st = a > cache_stages ? a : cache_stages; st < z; ++st) {
+      const int t0 = ((st - cache_stages) * SP + team) * 32;  // first node of the team's step
       __syncthreads();
-      uint8_t* kv = s_kv[0];
-      for (int e = tid; e < 32 * (D / 8); e += TT) {
+      uint8_t* kv = s_kv[0][team];
+      for (int e = tt; e < 32 * (D / 8); e += TT) {
         const int t = e / (D / 8), ch = e - t * (D / 8);
         u32x4 kx{0u, 0u, 0u, 0u}, vx{0u, 0u, 0u, 0u};
         if (t0 + t < nodes) {
@@ -280,40 +300,65 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
       }
       __syncthreads();
       const TreeScale one{p.scale_log2, 0.f, 1.f, 1.f};
-      if (active) consume(0, true, (uint32_t)(sees >> t0), one, one);
+      if (active && t0 < nodes) consume(0, true, (uint32_t)(sees >> t0), one, one);
     }
 
-    // The piece's result: the rows, or one partial.
-    const float l_tot = sum_xor32(l_run);
-    if (a == 0 && z == sq.stages) {
-      if (mine) {
-        const bool none = L == 0 && sees == 0;  // nothing to attend: zeros
-        const float inv = none ? 0.f : 1.f / l_tot;
-        uint16_t* o = p.out + row * D;
+    // The piece's result: a tile's SP waves merged in LDS, each summing a share of the quads;
+    // then the rows, or one partial.
+    constexpr int QUADS = 4 * DB;
+    float S = sum_xor32(l_run), M = m_run;
+    f32x4* s_o = (f32x4*)&s_kv[0][0][0];  // [wave][quad][lane]
+    if constexpr (SP > 1) {
+      __syncthreads();  // the buffers are free
+      if (h == 0) s_ml[wave][col] = make_float2(m_run, S);
+      __syncthreads();
 #pragma unroll
-        for (int i = 0; i < DB; ++i)
+      for (int w = 0; w < SP; ++w) M = fmaxf(M, s_ml[w * NT + tile][col].x);
+      S = 0.f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            *(bf16x4*)(o + 32 * i + 8 * j + 4 * h) = bf16x4{
-                (__bf16)(acc[i][4 * j] * inv), (__bf16)(acc[i][4 * j + 1] * inv),
-                (__bf16)(acc[i][4 * j + 2] * inv), (__bf16)(acc[i][4 * j + 3] * inv)};
+      for (int w = 0; w < SP; ++w) {
+        const float2 ml = s_ml[w * NT + tile][col];
+        S += ml.y * (ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M));
       }
-    } else {
-      const int64_t slot = 2 * (int64_t)blockIdx.x + (first_piece ? 0 : 1);
-      if (active) {
-        f32x4* po = (f32x4*)(p.part_o + (slot * NT + wave) * 32 * D);
+      const float f = m_run == M ? 1.f : __builtin_amdgcn_exp2f(m_run - M);
 #pragma unroll
-        for (int i = 0; i < DB; ++i)
+      for (int i = 0; i < DB; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            po[(4 * i + j) * 64 + lane] = f32x4{acc[i][4 * j], acc[i][4 * j + 1],
-                                                acc[i][4 * j + 2], acc[i][4 * j + 3]};
-        if (h == 0) p.part_ml[(slot * NT + wave) * 32 + col] = make_float2(m_run, l_tot);
-      }
-      if (a == 0 && tid == 0)
-        p.cuts[blockIdx.x] = make_int4(b, g * sq.blocks + blk,
-                                       tree_pieces(rg, x + taken + (sq.stages - z) - 1), (int)slot);
+        for (int j = 0; j < 4; ++j)
+          s_o[(wave * QUADS + 4 * i + j) * 64 + lane] =
+              f32x4{acc[i][4 * j] * f, acc[i][4 * j + 1] * f, acc[i][4 * j + 2] * f,
+                    acc[i][4 * j + 3] * f};
+      __syncthreads();
     }
+    const bool whole = a == 0 && z == sq.stages;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (first_piece ? 0 : 1);
+    const bool none = L == 0 && sees == 0;  // nothing to attend: zeros
+    const float inv = none ? 0.f : 1.f / S;
+#pragma unroll
+    for (int k = 0; k < QUADS / SP; ++k) {
+      const int quad = team + SP * k, i = quad >> 2, j = quad & 3;
+      f32x4 o;
+      if constexpr (SP > 1) {
+        o = s_o[(tile * QUADS + quad) * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < SP; ++w) o += s_o[((w * NT + tile) * QUADS + quad) * 64 + lane];
+      } else {
+        o = f32x4{acc[k >> 2][4 * (k & 3)], acc[k >> 2][4 * (k & 3) + 1], acc[k >> 2][4 * (k & 3) + 2],
+                  acc[k >> 2][4 * (k & 3) + 3]};
+      }
+      if (!whole) {
+        if (active) ((f32x4*)(p.part_o + (slot * NT + tile) * 32 * D))[quad * 64 + lane] = o;
+      } else if (mine) {
+        *(bf16x4*)(p.out + row * D + 32 * i + 8 * j + 4 * h) =
+            bf16x4{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv),
+                   (__bf16)(o[3] * inv)};
+      }
+    }
+    if (!whole && active && team == 0 && h == 0)
+      p.part_ml[(slot * NT + tile) * 32 + col] = make_float2(M, S);
+    if (!whole && a == 0 && tid == 0)
+      p.cuts[blockIdx.x] = make_int4(b, g * sq.blocks + blk,
+                                     tree_pieces(rg, x + taken + (sq.stages - z) - 1), (int)slot);
     if (p.whole) return;
     x += taken;
     if (x >= rg.x1) return;  // uniform
@@ -368,14 +413,21 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeParams p) {
   }
 }
 
-hipError_t launch_tree_wide(const TreeParams& p, int D, int P, bool fp8, int64_t grid, hipStream_t s) {
+template <int D, int P, bool FP8>
+static const void* wide_fn(int tiles) {
+  return tiles == 2 ? (const void*)&tree_kernel<D, P, FP8, 2>
+                    : (const void*)&tree_kernel<D, P, FP8, kTreeTiles>;
+}
+
+hipError_t launch_tree_wide(const TreeParams& p, int D, int P, bool fp8, int tiles, int64_t grid,
+                            hipStream_t s) {
   const void* fn;
   if (D == 128)
-    fn = P == 16 ? (fp8 ? (const void*)&tree_kernel<128, 16, true> : (const void*)&tree_kernel<128, 16, false>)
-                 : (fp8 ? (const void*)&tree_kernel<128, 32, true> : (const void*)&tree_kernel<128, 32, false>);
+    fn = P == 16 ? (fp8 ? wide_fn<128, 16, true>(tiles) : wide_fn<128, 16, false>(tiles))
+                 : (fp8 ? wide_fn<128, 32, true>(tiles) : wide_fn<128, 32, false>(tiles));
   else
-    fn = P == 16 ? (fp8 ? (const void*)&tree_kernel<64, 16, true> : (const void*)&tree_kernel<64, 16, false>)
-                 : (fp8 ? (const void*)&tree_kernel<64, 32, true> : (const void*)&tree_kernel<64, 32, false>);
+    fn = P == 16 ? (fp8 ? wide_fn<64, 16, true>(tiles) : wide_fn<64, 16, false>(tiles))
+                 : (fp8 ? wide_fn<64, 32, true>(tiles) : wide_fn<64, 32, false>(tiles));
   TreeParams arg = p;
   void* args[] = {(void*)&arg};
   const unsigned lds = p.whole ? 0 : (unsigned)(p.num_seqs + 1) * 4;

@@ -130,14 +130,23 @@ __device__ __forceinline__ TreeScale tree_scale(float scale_log2, float k_scale,
   }
 }
 
-// A step over 32 tokens for a tile of 32 columns: S^T = K Q^T, online softmax in the log2
-// domain, O^T += V^T P^T.  Lane (column lane & 31, half h = lane >> 5) holds in its
+// Weights above this (as a sum over a lane's 16 tokens) make a column's reference move up to
+// its maximum.
+constexpr float kTreeMostWeight = 256.f;
+
+// A step over 32 tokens for a tile of 32 columns: S^T = K Q^T, softmax weights 2^(s - m) of
+// the log2 domain, O^T += V^T P^T.  Lane (column lane & 31, half h = lane >> 5) holds in its
 // registers 8s + e the scores of the 8 tokens that it supplies to k-step s of the second
 // product.  kf(ks): K operand of 16 head-dim values; vf(i, s): V operand of head-dim rows
 // 32i .. 32i + 31 and k-step s.  s0, s1: the scales of registers 0-7 and 8-15.  bits: the
 // registers that count for the lane's column, where some does not (masked, uniform: a
 // branch around the scores alone, as a second copy of the step would need registers for a
 // second set of accumulators).
+//   m is a reference and not the running maximum: it moves only where the weights grow past
+// kTreeMostWeight, so that most steps neither look for their maximum nor rescale (96 of 175
+// vector instructions a step, the matrix products apart).  The weights are rounded to bf16
+// for the second product, and their sum is taken over the rounded ones: what the rounding
+// does to a row's largest weight then cancels.
 //   AHEAD: the operands come from LDS.  All of K's are read before the first product and
 // all of V's before the softmax, so that the reads' latency is waited for once, and the
 // second time behind the softmax (the compiler by itself reads two ahead).
@@ -168,28 +177,41 @@ __device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale 
     for (int k = 0; k < KS; ++k) op[k] = vf(k >> 1, k & 1);
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (FP8 && !(s0.mul > 0.f && s1.mul > 0.f)) {  // uniform: the maximum below needs mul > 0
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] *= r < 8 ? s0.mul : s1.mul;
-    s0.mul = s1.mul = 1.f;
-  }
-  if (masked)
+  if (masked) {
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      if (!((bits >> r) & 1u)) sc[r] = -__builtin_inff();
-  float mx = sc[0], mx1 = sc[8];
-#pragma unroll
-  for (int r = 1; r < 8; ++r) {
-    mx = fmaxf(mx, sc[r]);
-    mx1 = fmaxf(mx1, sc[8 + r]);
+      sc[r] = (bits >> r) & 1u
+                  ? (r < 8 ? __builtin_fmaf(sc[r], s0.mul, s0.add) : __builtin_fmaf(sc[r], s1.mul, s1.add))
+                  : -__builtin_inff();
+    s0.mul = s1.mul = 1.f;
+    s0.add = s1.add = 0.f;
   }
-  if constexpr (FP8)
-    mx = fmaxf(__builtin_fmaf(mx, s0.mul, s0.add), __builtin_fmaf(mx1, s1.mul, s1.add));
-  else
-    mx = fmaxf(mx, mx1) * s0.mul;
-  mx = max_xor32(mx);
-  if (__ballot(mx > m_run)) {  // some column's maximum grows: rescale the tile
-    const float m_new = fmaxf(m_run, mx);
+  const float mul0 = s0.mul, mul1 = FP8 ? s1.mul : s0.mul;
+  const float add0 = FP8 ? s0.add : 0.f, add1 = FP8 ? s1.add : 0.f;
+  bf16x8 pb[2];
+  float sum[2];
+  auto weigh = [&]() {
+    const float b0 = add0 - m_run, b1 = add1 - m_run;
+    sum[0] = sum[1] = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const bf16x2 w{
+          (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], r < 8 ? mul0 : mul1, r < 8 ? b0 : b1)),
+          (__bf16)__builtin_amdgcn_exp2f(
+              __builtin_fmaf(sc[r + 1], r < 8 ? mul0 : mul1, r < 8 ? b0 : b1))};
+      sum[r >> 3] = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum[r >> 3],
+                                                    false);
+      pb[r >> 3][r & 7] = w[0];
+      pb[r >> 3][(r & 7) + 1] = w[1];
+    }
+  };
+  weigh();
+  if (__ballot(!(sum[0] + sum[1] <= kTreeMostWeight))) {
+    float mx = -__builtin_inff();
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      mx = fmaxf(mx, __builtin_fmaf(sc[r], r < 8 ? mul0 : mul1, r < 8 ? add0 : add1));
+    const float m_new = fmaxf(m_run, max_xor32(mx));
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
     m_run = m_new;
     l_run *= alpha;
@@ -197,26 +219,17 @@ __device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale 
     for (int i = 0; i < DB; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
-  }
-  const float b0 = FP8 ? s0.add - m_run : -m_run, b1 = FP8 ? s1.add - m_run : -m_run;
-  float sum[2] = {0.f, 0.f};
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    sc[r] = __builtin_amdgcn_exp2f(
-        __builtin_fmaf(sc[r], FP8 && r >= 8 ? s1.mul : s0.mul, r < 8 ? b0 : b1));
-    sum[r >> 3] += sc[r];
+    weigh();
   }
   if constexpr (FP8) {
     l_run = __builtin_fmaf(sum[0], s0.inv, __builtin_fmaf(sum[1], s1.inv, l_run));
     if (s0.left != 1.f || s1.left != 1.f)  // uniform
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] *= r < 8 ? s0.left : s1.left;
+      for (int r = 0; r < 16; ++r)
+        pb[r >> 3][r & 7] = (__bf16)((float)pb[r >> 3][r & 7] * (r < 8 ? s0.left : s1.left));
   } else {
     l_run += sum[0] + sum[1];
   }
-  bf16x8 pb[2];
-#pragma unroll
-  for (int r = 0; r < 16; ++r) pb[r >> 3][r & 7] = (__bf16)sc[r];
 #pragma unroll
   for (int i = 0; i < DB; ++i)
 #pragma unroll

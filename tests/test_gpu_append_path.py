@@ -134,6 +134,44 @@ def test_equals_single_appends(dt):
             assert torch.equal(x.view(dtype), y.view(dtype))
 
 
+@pytest.mark.parametrize("scale", [float("nan"), 0.0, 2.0 ** -126, 2.0 ** -81, 2.0 ** -80 * 1.3, 2.0 ** -40, (5 * 2 ** 20 - 1) * 2.0 ** -23,
+                                   (9 * 2 ** 20 + 1) * 2.0 ** -30, 0.75, 1.0, 2.0 ** 60 * 1.7, 2.0 ** 99, 2.0 ** 101, float("inf")])
+def test_every_magnitude_over_every_scale(scale):
+    """Against dora_kv_append: random bit patterns under a page scale that is given, quotients next to
+    and on the ties of two codes, zeros of both signs, and what is far below or above the scale."""
+    D = lib()
+    g = torch.Generator().manual_seed(3)
+    B, T, Hkv, d, P = 24, 15, 4, 128, 16
+    k, v, ks, vs = _pool(2 * B, Hkv, d, P, 1, g)
+    s = scale if 0 < scale < 1e38 else 1.0
+    ks[:], vs[:] = scale, scale
+    new = []
+    for _ in range(2):
+        ties = (torch.randint(0, 512, (B, T, Hkv, d), generator=g).double() - 256) * s * 2.0 ** torch.randint(-8, 1, (B, T, Hkv, d), generator=g).double()
+        wide = torch.randn(B, T, Hkv, d, generator=g).double() * s * 2.0 ** torch.randint(-20, 7, (B, T, 1, 1), generator=g).double()
+        x = torch.where(torch.rand(B, T, Hkv, d, generator=g) < 0.5, ties, wide).to(torch.bfloat16)
+        bits = torch.randint(0, 65536, x.shape, generator=g, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+        x = torch.where(torch.rand(B, T, 1, 1, generator=g) < 0.05, bits, x)
+        new.append(torch.where(torch.rand(x.shape, generator=g) < 0.02, x * 0, x).cuda())
+    bt = torch.randperm(2 * B, generator=g).to(torch.int32).view(B, 2).cuda()
+    before = (torch.arange(B, dtype=torch.int32) % 17).cuda()
+    pools = [[x.cuda() for x in (k, v, ks, vs)] for _ in range(2)]
+    kw = dict(num_kv_heads=Hkv, page_size=P, kv_dtype=1)
+    for i in range(T):
+        a = pools[0]
+        D.dora_kv_append(new[0][:, i].contiguous(), new[1][:, i].contiguous(), bt, before + i + 1, a[0], a[1], k_scales=a[2], v_scales=a[3], **kw)
+    a = pools[1]
+    D.dora_kv_append_path(new[0], new[1], bt, before + T, a[0], a[1], k_scales=a[2], v_scales=a[3], **kw)
+    torch.cuda.synchronize()
+    for x, y in zip(*pools):
+        if x.element_size() == 1:
+            # apart from a NaN code's sign: under a NaN scale the old code's value is a product of two
+            # NaNs, whose sign IEEE 754 leaves open
+            assert _same(x.cpu().numpy(), y.cpu().numpy(), 1)
+        else:
+            assert torch.equal(x.view(torch.int32), y.view(torch.int32))
+
+
 def test_infinities_and_nan():
     def odd(kn, vn):
         kn[0, 2, 0, 5] = float("inf")

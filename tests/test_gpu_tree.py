@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from cache_util import Cache, check, random_trees, tree_reference
+from cache_util import Cache, check, odd_scales, random_trees, tree_reference
 from gpu_util import lib
 
 pytestmark = pytest.mark.gpu
@@ -99,6 +99,20 @@ def test_masks_that_leave_rows_empty():
     got = _case([0, 0, 5, 0], [T, T, T, T], T, 1, 2, 64, 16, 0, seed=12, masks=masks)
     assert torch.all(got[0] == 0) and torch.all(got[3, 1::2] == 0)
     _case([0, 700, 5, 0], [T, T, T, T], T, 1, 2, 64, 32, 1, seed=13, masks=masks, stride=60)
+
+
+@pytest.mark.parametrize("P", [16, 32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,G", [(4, 4), (12, 4), (16, 8)])
+def test_odd_scales(d, P, T, G):
+    c = Cache([300, 100, 90, 211, 64, 50, 33], 2, d, P, 1, seed=d + P)
+    odd_scales(c)
+    ns = [T, T, 1, T - 1, T, 2, T]
+    mask = random_trees(np.random.default_rng(T), ns, T)
+    q, kd, vd = _drafts(7, T, 2, G, d, ns, T)
+    out = torch.full((7, T, 2 * G, d), 7.0, dtype=torch.bfloat16)
+    want, spread = tree_reference(c, q, kd, vd, mask, ns, out)
+    check(_run(c, q, kd, vd, mask, ns, out), want, spread, "tree", roundings=2)
 
 
 def test_infinite_scores():

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from cache_util import Cache, check, window_reference
+from cache_util import Cache, check, odd_scales, window_reference
 from gpu_util import lib
 
 pytestmark = pytest.mark.gpu
@@ -81,6 +81,21 @@ def test_window_past_every_row_is_the_plain_decode():
         want, spread = window_reference(c, q.cpu(), 640, 0)
         check(out, want, spread)
         check(plain, want, spread)
+
+
+@pytest.mark.parametrize("P", [16, 32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 150])
+def test_odd_scales(d, P, n):
+    """n = 150: more segments than the steps over two pages take."""
+    c = Cache([300, 100, 90, 211, 64, 50, 33] * n, 4, d, P, 1, seed=d + P)
+    odd_scales(c)
+    q = _q(7 * n, 8, d, P)
+    want, spread = window_reference(c, q, 70, 20)
+    dev = c.gpu()
+    out = torch.empty_like(q).cuda()
+    lib().dora_decode_attn_window(q.cuda(), dev["k"], dev["v"], dev["bt"], dev["lens"], None, out, window=70, sinks=20, **dev["kw"])
+    check(out, want, spread, "window", roundings=2)
 
 
 def test_infinite_scores():

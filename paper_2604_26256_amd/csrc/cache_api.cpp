@@ -224,7 +224,7 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
     const int64_t grid =
         p.whole ? (int64_t)p.num_seqs * d.num_kv_heads * t.blocks : t.workgroups;
     const hipError_t e =
-        t.tiles < 2 ? launch_tree_narrow(p, d.head_dim, d.page_size, fp8, t.tiles, grid, s)
+        t.tiles < 2 ? launch_tree_narrow(p, d.head_dim, d.page_size, fp8, grid, s)
                      : launch_tree_wide(p, d.head_dim, d.page_size, fp8, t.tiles, grid, s);
     if (e != hipSuccess) return DORA_ERR_HIP;
     if (!p.whole && launch_tree_combine(p, d.head_dim, t.tiles, grid, s) != hipSuccess)

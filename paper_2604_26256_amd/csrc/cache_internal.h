@@ -41,8 +41,8 @@ struct TreeParams {
   float scale_log2;
 };
 
-// Up to two tiles (tree_narrow.hip), or blocks of four (tree.hip).
-hipError_t launch_tree_narrow(const TreeParams& p, int head_dim, int page_size, bool fp8, int tiles,
+// One tile (tree_narrow.hip), or two or blocks of four (tree.hip).
+hipError_t launch_tree_narrow(const TreeParams& p, int head_dim, int page_size, bool fp8,
                               int64_t grid, hipStream_t s);
 hipError_t launch_tree_wide(const TreeParams& p, int head_dim, int page_size, bool fp8, int tiles,
                             int64_t grid, hipStream_t s);

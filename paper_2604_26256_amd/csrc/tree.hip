@@ -369,48 +369,61 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
 }
 
 // Joins the pieces of the cut segment whose first piece workgroup blockIdx.x had: tile
-// blockIdx.y.  Thread t holds accumulator quads t >> 6, (t >> 6) + 4, ... of lane t & 63.
+// blockIdx.y, accumulator quads 4 blockIdx.z .. + 3 (rows 32 blockIdx.z .. + 31 of the head's
+// dim), one a wave.  A read of the partials, little else: many small workgroups, and the
+// loads of kTreeJoin pieces at a time.
+constexpr int kTreeJoin = 4;
 template <int D, int NT>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeParams p) {
-  constexpr int DB = D / 32, CB = 32 * NT;
+  constexpr int CB = 32 * NT;
   const int4 cut = p.cuts[blockIdx.x];
   if (cut.x < 0) return;
   const int b = cut.x, tile = blockIdx.y, lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const TreeSeq sq = tree_seq(p, b, 32, 1, CB);  // (only nodes, blocks and L > 0 matter here)
-  const int g = cut.y / sq.blocks, blk = cut.y - g * sq.blocks;
-  if (blk * CB + tile * 32 >= sq.nodes * p.group) return;  // no such columns
+  const int j = threadIdx.x >> 6, quad = 4 * blockIdx.z + j;
   float M = -__builtin_inff(), S = 0.f;
-  f32x4 acc[DB];
+  f32x4 acc{0.f, 0.f, 0.f, 0.f}, o[kTreeJoin];
+  float2 ml[kTreeJoin];
+  auto load = [&](int k0) {
 #pragma unroll
-  for (int i = 0; i < DB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < cut.z; ++k) {
-    const int64_t slot = k == 0 ? cut.w : 2 * ((int64_t)blockIdx.x + k);
-    const float2 ml = p.part_ml[(slot * NT + tile) * 32 + col];
-    const f32x4* po = (const f32x4*)(p.part_o + (slot * NT + tile) * 32 * D);
-    f32x4 o[DB];
-#pragma unroll
-    for (int i = 0; i < DB; ++i) o[i] = po[((threadIdx.x >> 6) + 4 * i) * 64 + lane];
-    const float m = fmaxf(M, ml.x);
-    const float f0 = M == m ? 1.f : __builtin_amdgcn_exp2f(M - m);
-    const float f1 = ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
-    M = m;
-    S = S * f0 + ml.y * f1;
-#pragma unroll
-    for (int i = 0; i < DB; ++i) acc[i] = acc[i] * f0 + o[i] * f1;
-  }
+    for (int k = 0; k < kTreeJoin; ++k) {  // past the end the last piece's again
+      const int at = k0 + k < cut.z ? k0 + k : cut.z - 1;
+      const int64_t slot = at == 0 ? cut.w : 2 * ((int64_t)blockIdx.x + at);
+      ml[k] = p.part_ml[(slot * NT + tile) * 32 + col];
+      o[k] = ((const f32x4*)(p.part_o + (slot * NT + tile) * 32 * D))[quad * 64 + lane];
+    }
+  };
+  load(0);  // beside the sequence's lengths
+  __builtin_amdgcn_sched_barrier(0);
+  const int g = cut.y / sq.blocks, blk = cut.y - g * sq.blocks;
   const int c = blk * CB + tile * 32 + col, node = c / p.group, head = c - node * p.group;
-  if (node >= sq.nodes) return;
+  if (blk * CB + tile * 32 >= sq.nodes * p.group) return;  // no such columns
   const uint64_t live = sq.nodes >= 64 ? ~0ull : (1ull << sq.nodes) - 1;
-  const bool none = sq.L == 0 && (p.tree_mask[(int64_t)b * p.num_nodes + node] & live) == 0;
+  const bool mine = node < sq.nodes;
+  const bool none = sq.L == 0 && mine && (p.tree_mask[(int64_t)b * p.num_nodes + node] & live) == 0;
+  for (int k0 = 0; k0 < cut.z; k0 += kTreeJoin) {
+    if (k0 > 0) load(k0);
+    float m = M;
+#pragma unroll
+    for (int k = 0; k < kTreeJoin; ++k) m = fmaxf(m, ml[k].x);
+    const float f0 = M == m ? 1.f : __builtin_amdgcn_exp2f(M - m);
+    M = m;
+    S *= f0;
+    acc *= f0;
+#pragma unroll
+    for (int k = 0; k < kTreeJoin; ++k) {
+      if (k0 + k >= cut.z) break;  // uniform
+      const float f = ml[k].x == m ? 1.f : __builtin_amdgcn_exp2f(ml[k].x - m);
+      S += ml[k].y * f;
+      acc += o[k] * f;
+    }
+  }
+  if (!mine) return;
   const float inv = none ? 0.f : 1.f / S;
   uint16_t* out = p.out + (((int64_t)b * p.num_nodes + node) * p.num_q_heads + g * p.group + head) * D;
-#pragma unroll
-  for (int k = 0; k < DB; ++k) {
-    const int quad = (threadIdx.x >> 6) + 4 * k, i = quad >> 2, j = quad & 3;
-    *(bf16x4*)(out + 32 * i + 8 * j + 4 * h) =
-        bf16x4{(__bf16)(acc[k][0] * inv), (__bf16)(acc[k][1] * inv), (__bf16)(acc[k][2] * inv),
-               (__bf16)(acc[k][3] * inv)};
-  }
+  *(bf16x4*)(out + 32 * blockIdx.z + 8 * j + 4 * h) =
+      bf16x4{(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv),
+             (__bf16)(acc[3] * inv)};
 }
 
 template <int D, int P, bool FP8>
@@ -446,7 +459,7 @@ hipError_t launch_tree_combine(const TreeParams& p, int D, int tiles, int64_t gr
                       : (const void*)&tree_combine_kernel<64, kTreeTiles>;
   TreeParams arg = p;
   void* args[] = {(void*)&arg};
-  return hipLaunchKernel(fn, dim3((unsigned)grid, (unsigned)tiles), dim3(256), args, 0, s);
+  return hipLaunchKernel(fn, dim3((unsigned)grid, (unsigned)tiles, (unsigned)(D / 32)), dim3(256), args, 0, s);
 }
 
 }  // namespace dora

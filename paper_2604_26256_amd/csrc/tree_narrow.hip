@@ -1,7 +1,5 @@
-// Tree attention for few columns (nodes x group) per KV head: a tile of 32 columns per
-// wave, a team of as many waves as there are tiles, and the teams take a workgroup's
-// steps in turn.  A wave loads its steps straight from HBM into matrix operands; the
-// waves of a team read the same lines, which come out of the caches but for the first.
+// Tree attention for at most 32 columns (nodes x group) per KV head, a tile: the waves of a
+// workgroup take its steps in turn, and load them straight from HBM into matrix operands.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -42,14 +40,14 @@ struct TreeRegs {
   vraw_t v[NV];
 };
 
-template <bool NT, typename T>
+template <typename T>
 __device__ __forceinline__ T tree_load(const uint8_t* at) {
-  return NT ? __builtin_nontemporal_load((const T*)at) : *(const T*)at;
+  return __builtin_nontemporal_load((const T*)at);
 }
 
-template <int D, int P, bool FP8, int TEAM>
+template <int D, int P, bool FP8>
 __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_narrow_kernel(TreeParams p) {
-  constexpr int SP = kTreeWaves / TEAM, PAIR = 32 / P, CB = 32 * TEAM;
+  constexpr int SP = kTreeWaves, PAIR = 32 / P;
   constexpr int KS = D / 16, DB = D / 32, E = FP8 ? 1 : 2;
   constexpr int TILE = P * D * E;  // bytes of one (page, KV head) tile
   constexpr int QUADS = 4 * DB;    // accumulator quads of a tile
@@ -61,7 +59,6 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
-  const int team = wave / TEAM, tile = wave % TEAM;
   const int Hkv = p.num_kv_heads, G = p.group;
 
   TreeRange rg{0, 0, 0, 1, 0};
@@ -69,7 +66,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
   if (p.whole) {
     b = (int)blockIdx.x / Hkv;
   } else {
-    rg = tree_range<P, SP, CB, kTreeNarrowCost>(p, s_pre);
+    rg = tree_range<P, SP, 32, kTreeNarrowCost>(p, s_pre);
     if (tid == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if (rg.x0 >= rg.x1) return;  // uniform
     b = rg.b;
@@ -86,7 +83,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
   int x = rg.x0;
   while (true) {
     // the piece: stages a .. z - 1 of (b, g)
-    const TreeSeq sq = tree_seq(p, b, P, SP, CB);
+    const TreeSeq sq = tree_seq(p, b, P, SP, 32);
     int g, a, z, taken = 0;
     if (p.whole) {
       g = (int)blockIdx.x - b * Hkv;
@@ -113,8 +110,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     const int L = uni(sq.L), nodes = uni(sq.nodes), n_pages = uni(sq.pages);
     const int cache_steps = uni(sq.cache_steps), cache_stages = uni(sq.cache_stages);
 
-    // this team's steps of the cache: st0, st0 + SP, ...; lane u holds the pages of its u-th
-    const int st0 = a * SP + team;
+    // this wave's steps of the cache: st0, st0 + SP, ...; lane u holds the pages of its u-th
+    const int st0 = a * SP + wave;
     const int c_end = z < cache_stages ? z * SP : cache_steps;  // past the piece's last step
     int steps = c_end > st0 ? (c_end - st0 + SP - 1) / SP : 0;
     const int32_t* row_ids = p.block_table + (int64_t)b * p.stride;
@@ -129,7 +126,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
 
     // query operand and mask: this lane's column.  fp8: a lane's 16-byte K piece is 16 head-dim
     // values, its k-steps 2m and 2m + 1.
-    const int c = 32 * tile + col, node = c / G, head = c - node * G;
+    const int node = col / G, head = col - node * G;
     const bool mine = node < nodes;
     const int64_t row = (((int64_t)b * p.num_nodes + (mine ? node : 0)) * p.num_q_heads +
                          (int64_t)g * G + (mine ? head : 0));
@@ -145,7 +142,6 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
 #pragma unroll
       for (int s = 0; s < KS; ++s) qop[s] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
     }
-    if (32 * tile >= nodes * G) steps = 0;  // uniform: the wave's tile has no columns
 
     f32x16 acc[DB];
     float m_run = kNoMax, l_run = 0.f;
@@ -176,7 +172,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
         const uint8_t* kb = p.k_pages + (ksecond ? base1 : base0) + (past ? 0u : koff);
 #pragma unroll
         for (int s = 0; s < R::NK; ++s)
-          buf[r].k[s] = tree_load<TEAM == 1, u32x4>(kb + s * (2 * P * 16));
+          buf[r].k[s] = tree_load<u32x4>(kb + s * (2 * P * 16));
         const uint8_t* vb0 = p.v_pages + base0 + (past ? 0u : voff);
         const uint8_t* vb1 = p.v_pages + base1 + (past ? 0u : voff);
 #pragma unroll
@@ -184,13 +180,13 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
           typedef typename R::vraw_t V;
           constexpr int BLK = 32 * P * E;  // bytes between 32-row blocks
           if constexpr (R::RUN16) {
-            buf[r].v[i] = tree_load<TEAM == 1, V>(vb0 + i * BLK);
+            buf[r].v[i] = tree_load<V>(vb0 + i * BLK);
           } else if constexpr (PAIR == 2) {
-            buf[r].v[2 * i] = tree_load<TEAM == 1, V>(vb0 + i * BLK);
-            buf[r].v[2 * i + 1] = tree_load<TEAM == 1, V>(vb1 + i * BLK);
+            buf[r].v[2 * i] = tree_load<V>(vb0 + i * BLK);
+            buf[r].v[2 * i + 1] = tree_load<V>(vb1 + i * BLK);
           } else {
-            buf[r].v[2 * i] = tree_load<TEAM == 1, V>(vb0 + i * BLK);
-            buf[r].v[2 * i + 1] = tree_load<TEAM == 1, V>(vb0 + i * BLK + 16 * E);
+            buf[r].v[2 * i] = tree_load<V>(vb0 + i * BLK);
+            buf[r].v[2 * i + 1] = tree_load<V>(vb0 + i * BLK + 16 * E);
           }
         }
       };
@@ -261,9 +257,9 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
 
     // Drafts (the last stages).  V is turned round through the wave's part of LDS.
     for (int st = a > cache_stages ? a : cache_stages; st < z; ++st) {
-      // the team with the fewest cache steps first
-      const int t0 = ((st - cache_stages) * SP + SP - 1 - team) * 32;
-      if (t0 >= nodes || 32 * tile >= nodes * G) continue;  // uniform in the wave
+      // the wave with the fewest cache steps first
+      const int t0 = ((st - cache_stages) * SP + SP - 1 - wave) * 32;
+      if (t0 >= nodes) continue;  // uniform in the wave
       uint8_t* vt = (uint8_t*)&s_o[wave][0][0];  // [d][32 nodes], pieces of 8 displaced by row
       auto v_at = [](int row_, int piece) { return row_ * 64 + ((piece ^ ((row_ >> 2) & 3)) << 4); };
       for (int e = lane; e < 32 * (D / 8); e += 64) {
@@ -290,54 +286,45 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
                         m_run, l_run);
     }
 
-    // The piece's result: a tile's SP waves merged in LDS, each summing a share of the quads;
-    // then the rows, or one partial.
+    // The piece's result: the waves' merged in LDS, each summing a share of the quads; then the
+    // rows, or one partial.
     const bool whole = a == 0 && z == sq.stages;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (first_piece ? 0 : 1);
     float S = sum_xor32(l_run), M = m_run;
-    if constexpr (SP > 1) {
-      if (h == 0) s_ml[wave][col] = make_float2(m_run, S);
-      __syncthreads();  // and every wave has done with its drafts
+    if (h == 0) s_ml[wave][col] = make_float2(m_run, S);
+    __syncthreads();  // and every wave has done with its drafts
 #pragma unroll
-      for (int w = 0; w < SP; ++w) M = fmaxf(M, s_ml[w * TEAM + tile][col].x);
-      S = 0.f;
+    for (int w = 0; w < SP; ++w) M = fmaxf(M, s_ml[w][col].x);
+    S = 0.f;
 #pragma unroll
-      for (int w = 0; w < SP; ++w) {
-        const float2 ml = s_ml[w * TEAM + tile][col];
-        S += ml.y * (ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M));
-      }
-      const float f = m_run == M ? 1.f : __builtin_amdgcn_exp2f(m_run - M);
-#pragma unroll
-      for (int i = 0; i < DB; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          s_o[wave][4 * i + j][lane] = f32x4{acc[i][4 * j] * f, acc[i][4 * j + 1] * f,
-                                             acc[i][4 * j + 2] * f, acc[i][4 * j + 3] * f};
-      __syncthreads();
+    for (int w = 0; w < SP; ++w) {
+      const float2 ml = s_ml[w][col];
+      S += ml.y * (ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M));
     }
+    const float f = m_run == M ? 1.f : __builtin_amdgcn_exp2f(m_run - M);
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        s_o[wave][4 * i + j][lane] = f32x4{acc[i][4 * j] * f, acc[i][4 * j + 1] * f,
+                                           acc[i][4 * j + 2] * f, acc[i][4 * j + 3] * f};
+    __syncthreads();
     const bool none = L == 0 && sees == 0;  // nothing to attend: zeros
     const float inv = none ? 0.f : 1.f / S;
 #pragma unroll
     for (int k = 0; k < QUADS / SP; ++k) {
-      const int quad = team + SP * k, i = quad >> 2, j = quad & 3;
-      f32x4 o;
-      if constexpr (SP > 1) {
-        o = s_o[tile][quad][lane];
+      const int quad = wave + SP * k, i = quad >> 2, j = quad & 3;
+      f32x4 o = s_o[0][quad][lane];
 #pragma unroll
-        for (int w = 1; w < SP; ++w) o += s_o[w * TEAM + tile][quad][lane];
-      } else {
-        o = f32x4{acc[k >> 2][4 * (k & 3)], acc[k >> 2][4 * (k & 3) + 1], acc[k >> 2][4 * (k & 3) + 2],
-                  acc[k >> 2][4 * (k & 3) + 3]};
-      }
+      for (int w = 1; w < SP; ++w) o += s_o[w][quad][lane];
       if (!whole)
-        ((f32x4*)(p.part_o + (slot * TEAM + tile) * 32 * D))[quad * 64 + lane] = o;
+        ((f32x4*)(p.part_o + slot * 32 * D))[quad * 64 + lane] = o;
       else if (mine)
         *(bf16x4*)(p.out + row * D + 32 * i + 8 * j + 4 * h) =
             bf16x4{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv),
                    (__bf16)(o[3] * inv)};
     }
-    if (!whole && team == 0 && h == 0)
-      p.part_ml[(slot * TEAM + tile) * 32 + col] = make_float2(M, S);
+    if (!whole && wave == 0 && h == 0) p.part_ml[slot * 32 + col] = make_float2(M, S);
     if (!whole && a == 0 && tid == 0)
       p.cuts[blockIdx.x] = make_int4(b, g, tree_pieces(rg, x + taken + (sq.stages - z) - 1), (int)slot);
     if (p.whole) return;
@@ -346,26 +333,18 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     first_piece = false;
     while (s_pre[b + 1] <= x) ++b;
     b = uni(b);
-    if constexpr (SP > 1) __syncthreads();  // s_o and s_ml: before the next piece's
+    __syncthreads();  // s_o and s_ml: before the next piece's
   }
 }
 
-template <int D, int P, bool FP8>
-static const void* narrow_fn(int tiles) {
-  return tiles == 1   ? (const void*)&tree_narrow_kernel<D, P, FP8, 1>
-         : tiles == 2 ? (const void*)&tree_narrow_kernel<D, P, FP8, 2>
-                      : (const void*)&tree_narrow_kernel<D, P, FP8, 4>;
+template <int D, int P>
+static const void* narrow_fn(bool fp8) {
+  return fp8 ? (const void*)&tree_narrow_kernel<D, P, true> : (const void*)&tree_narrow_kernel<D, P, false>;
 }
 
-hipError_t launch_tree_narrow(const TreeParams& p, int D, int P, bool fp8, int tiles, int64_t grid,
-                              hipStream_t s) {
-  const void* fn;
-  if (D == 128)
-    fn = P == 16 ? (fp8 ? narrow_fn<128, 16, true>(tiles) : narrow_fn<128, 16, false>(tiles))
-                 : (fp8 ? narrow_fn<128, 32, true>(tiles) : narrow_fn<128, 32, false>(tiles));
-  else
-    fn = P == 16 ? (fp8 ? narrow_fn<64, 16, true>(tiles) : narrow_fn<64, 16, false>(tiles))
-                 : (fp8 ? narrow_fn<64, 32, true>(tiles) : narrow_fn<64, 32, false>(tiles));
+hipError_t launch_tree_narrow(const TreeParams& p, int D, int P, bool fp8, int64_t grid, hipStream_t s) {
+  const void* fn = D == 128 ? (P == 16 ? narrow_fn<128, 16>(fp8) : narrow_fn<128, 32>(fp8))
+                            : (P == 16 ? narrow_fn<64, 16>(fp8) : narrow_fn<64, 32>(fp8));
   TreeParams arg = p;
   void* args[] = {(void*)&arg};
   const unsigned lds = p.whole ? 0 : (unsigned)(p.num_seqs + 1) * 4;

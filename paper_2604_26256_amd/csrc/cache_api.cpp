@@ -62,8 +62,7 @@ struct TreeLayout {
   size_t cuts_off, part_o_off, part_ml_off, total;
 };
 
-dora_status check_nodes(const dora_decode_desc& d, int32_t num_nodes) {
-  (void)d;
+dora_status check_nodes(int32_t num_nodes) {
   return num_nodes < 1 || num_nodes > 64 ? DORA_ERR_INVALID_ARG : DORA_OK;
 }
 
@@ -71,7 +70,8 @@ void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
   const int64_t columns = (int64_t)num_nodes * (d.num_q_heads / d.num_kv_heads);
   t->tiles = tree_tiles(columns);
   t->blocks = (int)((columns + 32 * t->tiles - 1) / (32 * t->tiles));
-  // A launch's stages (a segment's start counts as some) are counted in 32 bits.
+  // A launch's stages (a segment's start counts as some) are counted in 32 bits; one row's, of
+  // less than 2^19 pages, 128 heads and 9 blocks, always fit.
   const int64_t steps = ((int64_t)d.block_table_stride * d.page_size + 31) / 32 + 2 + 8;
   int64_t seqs = INT32_MAX / (steps * d.num_kv_heads * t->blocks);
   if (seqs > kTreeMaxSeqs) seqs = kTreeMaxSeqs;
@@ -91,13 +91,13 @@ void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
   t->total = off;
 }
 
-// Whether a launch takes a workgroup per (sequence, KV head, column block), uncut.
-bool tree_whole(const dora_decode_desc& d, const TreeLayout& t, int seqs) {
-  if (d.num_waves > 0) return false;
-  const int64_t tokens = (int64_t)d.block_table_stride * d.page_size;
-  (void)seqs;
-  (void)t;
-  return tokens <= 512;
+// Whether a launch takes a workgroup per (sequence, KV head, column block), uncut: where no row
+// is longer than 2,048 tokens.  Against equal ranges and their join (8 KV heads of 128 dims, fp8):
+// 128 rows of 400 tokens at the median, up to 2,048, 4 nodes, 43 us for 53; 256 rows of up to
+// 1,024 (4 heads, bf16, 8 nodes) 66 for 73; 8 of 1,024 (2 heads of 64, bf16) 10.2 for 12.5; but 4
+// full rows of 2,048 46 for 42, and of 4,096 (8 rows, 2 heads of 64) 23 for 17.
+bool tree_whole(const dora_decode_desc& d) {
+  return d.num_waves <= 0 && (int64_t)d.block_table_stride * d.page_size <= 2048;
 }
 
 // ---------------------------------------------------------------------------
@@ -160,7 +160,7 @@ dora_status validate_window(const dora_decode_desc& d, const int32_t* block_tabl
 extern "C" {
 
 size_t dora_decode_tree_workspace_bytes(const dora_decode_desc* desc, int32_t num_nodes) {
-  if (check_desc(desc) != DORA_OK || check_nodes(*desc, num_nodes) != DORA_OK) return 0;
+  if (check_desc(desc) != DORA_OK || check_nodes(num_nodes) != DORA_OK) return 0;
   TreeLayout t;
   tree_layout(*desc, num_nodes, &t);
   return t.total;
@@ -176,7 +176,7 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
   dora_status st = check_desc(desc);
   if (st != DORA_OK) return st;
   const dora_decode_desc& d = *desc;
-  st = check_nodes(d, num_nodes);
+  st = check_nodes(num_nodes);
   if (st != DORA_OK) return st;
   if (d.num_seqs == 0) return DORA_OK;
   st = check_attn(d, q, k_pages, v_pages, block_table, seq_lens, version_ids, out, workspace);
@@ -218,7 +218,7 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
     p.group = d.num_q_heads / d.num_kv_heads;
     p.stride = d.block_table_stride;
     p.blocks = t.blocks;
-    p.whole = tree_whole(d, t, p.num_seqs) ? 1 : 0;
+    p.whole = tree_whole(d) ? 1 : 0;
     p.page_bytes = page_bytes_of(d);
     p.scale_log2 = scale_log2_of(d);
     const int64_t grid =

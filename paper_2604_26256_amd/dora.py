@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 from typing import Optional, Sequence
 
 import numpy as np
@@ -631,14 +632,25 @@ def _call(device, stream, where, args):
     _check(getattr(_lib, where)(*args, _stream_handle(stream, device)), where)
 
 
-def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, cache, workspace):
+_thread = threading.local()  # workspaces of this thread's calls, by the call's name
+
+
+def _capturing(torch, stream):
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, workspace):
     """_call with a workspace of bytes_fn(args[0], *sizes) bytes after args (its size goes by the
-    device's compute units).  Without one given, the cached one of (device, stream); while a
-    graph is captured a new one, from the graph's own memory, so that no two graphs share one."""
+    device's compute units).  Without one given, the cached one of (thread, device, stream): two
+    threads' calls, of two launches each, may take turns on one stream.  While a graph is captured
+    a new one, from the graph's own memory, so that no two graphs share one."""
     torch = _torch()
     if torch._C._cuda_getDevice() != device.index:
         with torch.cuda.device(device):
-            return _call_with_workspace(device, stream, where, args, bytes_fn, sizes, cache, workspace)
+            return _call_with_workspace(device, stream, where, args, bytes_fn, sizes, workspace)
     need = int(getattr(_lib, bytes_fn)(args[0], *sizes))
     if need == 0:  # invalid or unsupported: let the library name the reason
         _call(device, stream, where, (*args, None, 0))
@@ -647,10 +659,11 @@ def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, cache, wo
         if workspace.device != device:
             raise ValueError(f"workspace is on {workspace.device}, tensors on {device}")
     else:
-        if torch.cuda.is_current_stream_capturing():
+        if _capturing(torch, stream):
             with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
                 workspace = torch.empty(need, dtype=torch.uint8, device=device)
         else:
+            cache = _thread.__dict__.setdefault(where, {})
             workspace = _cached_workspace(cache, device, stream, need)
         ptr, size = workspace.data_ptr(), need
     _call(device, stream, where, (*args, ptr, size))
@@ -662,10 +675,6 @@ def _scale_specs(k_scales, v_scales, page_owner, num_pages):
     return [(k_scales, "k_scales", (torch.float32,), (num_pages,), 4),
             (v_scales, "v_scales", (torch.float32,), (num_pages,), 4),
             (page_owner, "page_owner", (torch.int16,), (num_pages,), 2)]
-
-
-_tree_ws_cache = {}
-_window_ws_cache = {}
 
 
 def dora_decode_attn_tree(q, k_draft, v_draft, tree_mask, k_pages, v_pages, block_table, seq_lens,
@@ -715,7 +724,7 @@ def dora_decode_attn_tree(q, k_draft, v_draft, tree_mask, k_pages, v_pages, bloc
         *_scale_specs(k_scales, v_scales, page_owner, num_pages)])
     _call_with_workspace(q.device, stream, "dora_decode_attn_tree",
                          (ctypes.byref(desc), T, *ptrs[:11]), "dora_decode_tree_workspace_bytes",
-                         (T,), _tree_ws_cache, workspace)
+                         (T,), workspace)
     return out
 
 
@@ -760,8 +769,7 @@ def dora_decode_attn_window(q, k_pages, v_pages, block_table, seq_lens, version_
         *_scale_specs(k_scales, v_scales, page_owner, num_pages)])
     _call_with_workspace(q.device, stream, "dora_decode_attn_window",
                          (ctypes.byref(desc), window, sinks, *ptrs[:7]),
-                         "dora_decode_window_workspace_bytes", (window, sinks), _window_ws_cache,
-                         workspace)
+                         "dora_decode_window_workspace_bytes", (window, sinks), workspace)
     return out
 
 

@@ -222,6 +222,42 @@ def test_repeated_calls_streams_and_workspaces():
     assert e.value.status == D.DORA_ERR_WORKSPACE_TOO_SMALL
 
 
+def test_two_threads_on_one_stream():
+    """Calls of two launches each, from two threads on the same stream at once: each thread has a
+    workspace of its own."""
+    import threading
+    D = lib()
+    sets = []
+    for n in range(2):
+        c = Cache([3000 + 700 * n, 2100], 2, 64, 16, 0, seed=31 + n)
+        dev = c.gpu()
+        q, kd, vd = (x.cuda() for x in _drafts(2, 5, 2, 4, 64, [5] * 2, 33 + n))
+        mask = torch.from_numpy(random_trees(np.random.default_rng(n), [5] * 2, 5).view(np.int64)).cuda()
+        a = (q, kd, vd, mask, dev["k"], dev["v"], dev["bt"], dev["lens"], None)
+        want = D.dora_decode_attn_tree(*a, torch.empty_like(q), **dev["kw"])
+        sets.append((a, dev, want, [torch.empty_like(q) for _ in range(40)]))
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(a, dev, outs):
+        try:
+            for o in outs:
+                D.dora_decode_attn_tree(*a, o, **dev["kw"])
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(a, dev, outs)) for a, dev, _, outs in sets]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for _, _, want, outs in sets:
+        for o in outs:
+            assert torch.equal(o.view(torch.int16), want.view(torch.int16))
+
+
 def test_graph_replays():
     """Captured with the library's workspace, two graphs of different sizes, replayed in turn
     with new inputs between."""

@@ -61,13 +61,14 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
   const int team = wave / NT, tile = wave % NT, tt = tid - team * TT;
   const int Hkv = p.num_kv_heads, G = p.group;
 
+  const int place = tree_place(p);
   TreeRange rg{0, 0, 0, 1, 0};
   int b;
   if (p.whole) {
-    b = (int)blockIdx.x / (Hkv * p.blocks);
+    b = place / (Hkv * p.blocks);
   } else {
-    rg = tree_range<P, SP, CB, kTreeWideCost>(p, s_pre);
-    if (tid == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    rg = tree_range<P, SP, CB, kTreeWideCost>(p, place, s_pre);
+    if (tid == 0) p.cuts[place] = make_int4(-1, 0, 0, 0);
     if (rg.x0 >= rg.x1) return;  // uniform
     b = rg.b;
   }
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
     const TreeSeq sq = tree_seq(p, b, P, SP, CB);
     int g, blk, a, z, taken = 0;
     if (p.whole) {
-      const int r = (int)blockIdx.x - b * Hkv * p.blocks;
+      const int r = place - b * Hkv * p.blocks;
       g = r / p.blocks;
       blk = r - g * p.blocks;
       a = 0;
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
       __syncthreads();
     }
     const bool whole = a == 0 && z == sq.stages;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (first_piece ? 0 : 1);
+    const int64_t slot = 2 * (int64_t)place + (first_piece ? 0 : 1);
     const bool none = L == 0 && sees == 0;  // nothing to attend: zeros
     const float inv = none ? 0.f : 1.f / S;
 #pragma unroll
@@ -357,8 +358,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
     if (!whole && active && team == 0 && h == 0)
       p.part_ml[(slot * NT + tile) * 32 + col] = make_float2(M, S);
     if (!whole && a == 0 && tid == 0)
-      p.cuts[blockIdx.x] = make_int4(b, g * sq.blocks + blk,
-                                     tree_pieces(rg, x + taken + (sq.stages - z) - 1), (int)slot);
+      p.cuts[place] = make_int4(b, g * sq.blocks + blk,
+                                     tree_pieces(rg, place, x + taken + (sq.stages - z) - 1), (int)slot);
     if (p.whole) return;
     x += taken;
     if (x >= rg.x1) return;  // uniform
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
   }
 }
 
-// Joins the pieces of the cut segment whose first piece workgroup blockIdx.x had: tile
+// Joins the pieces of the cut segment whose first piece the workgroup of this place had: tile
 // blockIdx.y, accumulator quads 4 blockIdx.z .. + 3 (rows 32 blockIdx.z .. + 31 of the head's
 // dim), one a wave.  A read of the partials, little else: many small workgroups, and the
 // loads of kTreeJoin pieces at a time.
@@ -376,7 +377,8 @@ constexpr int kTreeJoin = 4;
 template <int D, int NT>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeParams p) {
   constexpr int CB = 32 * NT;
-  const int4 cut = p.cuts[blockIdx.x];
+  const int place = tree_place(p);
+  const int4 cut = p.cuts[place];
   if (cut.x < 0) return;
   const int b = cut.x, tile = blockIdx.y, lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const TreeSeq sq = tree_seq(p, b, 32, 1, CB);  // (only nodes, blocks and L > 0 matter here)
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeParams p) {
 #pragma unroll
     for (int k = 0; k < kTreeJoin; ++k) {  // past the end the last piece's again
       const int at = k0 + k < cut.z ? k0 + k : cut.z - 1;
-      const int64_t slot = at == 0 ? cut.w : 2 * ((int64_t)blockIdx.x + at);
+      const int64_t slot = at == 0 ? cut.w : 2 * ((int64_t)place + at);
       ml[k] = p.part_ml[(slot * NT + tile) * 32 + col];
       o[k] = ((const f32x4*)(p.part_o + (slot * NT + tile) * 32 * D))[quad * 64 + lane];
     }

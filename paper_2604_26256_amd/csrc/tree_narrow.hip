@@ -61,13 +61,14 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
   const int col = lane & 31, h = lane >> 5;
   const int Hkv = p.num_kv_heads, G = p.group;
 
+  const int place = tree_place(p);
   TreeRange rg{0, 0, 0, 1, 0};
   int b;
   if (p.whole) {
-    b = (int)blockIdx.x / Hkv;
+    b = place / Hkv;
   } else {
-    rg = tree_range<P, SP, 32, kTreeNarrowCost>(p, s_pre);
-    if (tid == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    rg = tree_range<P, SP, 32, kTreeNarrowCost>(p, place, s_pre);
+    if (tid == 0) p.cuts[place] = make_int4(-1, 0, 0, 0);
     if (rg.x0 >= rg.x1) return;  // uniform
     b = rg.b;
   }
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     const TreeSeq sq = tree_seq(p, b, P, SP, 32);
     int g, a, z, taken = 0;
     if (p.whole) {
-      g = (int)blockIdx.x - b * Hkv;
+      g = place - b * Hkv;
       a = 0;
       z = sq.stages;
       if (sq.nodes == 0) return;  // uniform
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     // The piece's result: the waves' merged in LDS, each summing a share of the quads; then the
     // rows, or one partial.
     const bool whole = a == 0 && z == sq.stages;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (first_piece ? 0 : 1);
+    const int64_t slot = 2 * (int64_t)place + (first_piece ? 0 : 1);
     float S = sum_xor32(l_run), M = m_run;
     if (h == 0) s_ml[wave][col] = make_float2(m_run, S);
     __syncthreads();  // and every wave has done with its drafts
@@ -326,7 +327,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     }
     if (!whole && wave == 0 && h == 0) p.part_ml[slot * 32 + col] = make_float2(M, S);
     if (!whole && a == 0 && tid == 0)
-      p.cuts[blockIdx.x] = make_int4(b, g, tree_pieces(rg, x + taken + (sq.stages - z) - 1), (int)slot);
+      p.cuts[place] = make_int4(b, g, tree_pieces(rg, place, x + taken + (sq.stages - z) - 1), (int)slot);
     if (p.whole) return;
     x += taken;
     if (x >= rg.x1) return;  // uniform

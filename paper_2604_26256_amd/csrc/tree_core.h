@@ -190,6 +190,7 @@ __device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale 
     __builtin_amdgcn_sched_barrier(0);
   }
   if (masked) {
+    asm volatile("" : "+v"(bits));  // (else the 16 tests are made before the branch, every step)
 #pragma unroll
     for (int r = 0; r < 16; ++r)
       sc[r] = (bits >> r) & 1u
@@ -235,11 +236,14 @@ __device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale 
   }
   if constexpr (FP8) {
     l_run = __builtin_fmaf(sum[0], s0.inv, __builtin_fmaf(sum[1], s1.inv, l_run));
-    if (s0.left != 1.f || s1.left != 1.f)  // uniform
+    if (s0.left != 1.f || s1.left != 1.f) {  // uniform
+      if (!masked) bits = 0xFFFFu;
+      asm volatile("" : "+v"(bits));
 #pragma unroll
       for (int r = 0; r < 16; ++r)  // (a weight that does not count stays 0 under an infinity)
-        if (!masked || ((bits >> r) & 1u))
+        if ((bits >> r) & 1u)
           pb[r >> 3][r & 7] = (__bf16)((float)pb[r >> 3][r & 7] * (r < 8 ? s0.left : s1.left));
+    }
   } else {
     l_run += sum[0] + sum[1];
   }

@@ -17,7 +17,7 @@
 
 namespace dora {
 
-// One step of T tokens, of which those with a bit in `bits` count: scores, online
+// A page of T tokens, of which those with a bit in `bits` count: scores, online
 // softmax and weighted values for one tile of 16 query columns, as the plain decode's
 // page step.  Values of tokens that do not count may be anything.  The V scale is folded into
 // the weights as in the tree step, whose reasons hold here too.
@@ -129,11 +129,11 @@ __device__ __forceinline__ uint32_t page_bits(int j, int L, int begin, int sinks
 }
 
 // One workgroup of kSegWaves waves per (sequence, KV head) segment, or per chunk of
-// p.chunk_pages of its visible pages.  Wave w takes steps w, w + kSegWaves, ... of T
-// tokens (a page of T, or two of 16); lane u holds the pages of the wave's u-th step.
-template <int D, int P, bool FP8, int T>
+// p.chunk_pages of its visible pages.  Wave w takes pages w, w + kSegWaves, ...; lane u holds the
+// id of the wave's u-th page.  (Two 16-token pages a step, as the plain decode has for few
+// segments, gain 3% for 16 segments of 512 tokens, 64 dims, nothing for 512, and lose 6% for 1,024.)
+template <int D, int P, bool FP8>
 __global__ __launch_bounds__(64 * kSegWaves, 2) void window_kernel(WindowParams p) {
-  constexpr int PAIR = T / P;
   constexpr int KSTEPS = D / 32, DBLK = D / 16;
   constexpr int TILE_BYTES = P * D * (FP8 ? 1 : 2);
   constexpr int ROW = D + 4;
@@ -154,7 +154,6 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void window_kernel(WindowParams 
   const int n_seg = vis.pages(), u0 = c * p.chunk_pages;
   if (c > 0 && u0 >= n_seg) return;  // uniform: the segment ends before this chunk
   const int n = n_seg - u0 < p.chunk_pages ? n_seg - u0 : p.chunk_pages;
-  const int n_steps = (n + PAIR - 1) / PAIR;
   const int Lc = (int64_t)L < (int64_t)p.stride * P ? L : p.stride * P;
   const int begin = Lc > p.window ? Lc - p.window : 0;
   auto page_at = [&](int u) { return u < vis.sink ? u : vis.first + (u - vis.sink); };
@@ -162,38 +161,30 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void window_kernel(WindowParams 
 #pragma unroll
   for (int i = 0; i < DBLK; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = kNoMax, l_run = 0.f;
-  const int steps = (n_steps - wave + kSegWaves - 1) / kSegWaves;  // <= 0: none for this wave
+  const int steps = (n - wave + kSegWaves - 1) / kSegWaves;  // <= 0: none for this wave
   if (steps > 0) {
-    // this lane's step of the wave: its pages (the last one past the end)
-    const int ul = PAIR * (wave + kSegWaves * lane);
-    const int32_t* row = p.block_table + (int64_t)b * p.stride;
-    const int j0 = page_at(u0 + (ul < n ? ul : n - 1));
-    const int j1 = page_at(u0 + (ul + 1 < n ? ul + 1 : n - 1));
-    int pid0 = row[j0];
-    int pid1 = PAIR == 2 ? row[j1] : 0;
-    int bits = (int)page_bits<P>(j0, Lc, begin, p.sinks);
-    if constexpr (PAIR == 2) {
-      if (ul + 1 < n) bits |= (int)(page_bits<P>(j1, Lc, begin, p.sinks) << 16);
-    }
-    const uint32_t koff = step_koff<D, P, T>(col, grp), voff = step_voff<D, P, FP8, T>(col, grp);
-    PageRegs<D, T, FP8> buf[2];
+    // this lane's page of the wave (the last one past the end)
+    const int ul = wave + kSegWaves * lane;
+    const int j = page_at(u0 + (ul < n ? ul : n - 1));
+    int pid = p.block_table[(int64_t)b * p.stride + j];
+    const int bits = (int)page_bits<P>(j, Lc, begin, p.sinks);
+    const uint32_t koff = step_koff<D, P, P>(col, grp), voff = step_voff<D, P, FP8, P>(col, grp);
+    PageRegs<D, P, FP8> buf[2];
     float s_ks[2] = {1.f, 1.f}, s_vs[2] = {1.f, 1.f};
     auto prefetch = [&](int r, int u) {
       const bool past = u >= steps;  // past the last step the loads still issue, one line each
       u = past ? steps - 1 : u;
-      const int p0 = __builtin_amdgcn_readlane(pid0, u);
-      const int p1 = PAIR == 2 ? __builtin_amdgcn_readlane(pid1, u) : p0;
+      const int page = __builtin_amdgcn_readlane(pid, u);
       if constexpr (FP8) {
-        s_ks[r] = PAIR == 2 && grp >= 2 ? p.k_scales[p1] : p.k_scales[p0];
-        s_vs[r] = PAIR == 2 && grp >= 2 ? p.v_scales[p1] : p.v_scales[p0];
+        s_ks[r] = p.k_scales[page];
+        s_vs[r] = p.v_scales[page];
       }
-      load_step<D, P, FP8, T, true>(buf[r], p.k_pages, p.v_pages,
-                                    (int64_t)p0 * p.page_bytes + (int64_t)g * TILE_BYTES,
-                                    (int64_t)p1 * p.page_bytes + (int64_t)g * TILE_BYTES,
-                                    past ? 0u : koff, past ? 0u : voff);
+      const int64_t at = (int64_t)page * p.page_bytes + (int64_t)g * TILE_BYTES;
+      load_step<D, P, FP8, P, true>(buf[r], p.k_pages, p.v_pages, at, at, past ? 0u : koff,
+                                    past ? 0u : voff);
     };
     // The table entries are waited for here, once.
-    asm volatile("" : "+v"(pid0), "+v"(pid1));
+    asm volatile("" : "+v"(pid));
     prefetch(0, 0);
     int u = 0;
     while (true) {
@@ -201,7 +192,7 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void window_kernel(WindowParams 
       for (int r = 0; r < 2; ++r) {
         prefetch(r ^ 1, u + 1);
         const uint32_t m = (uint32_t)__builtin_amdgcn_readlane(bits, u);
-        consume_bits<D, T, FP8>(buf[r], m, tree_scale<FP8>(p.scale_log2, s_ks[r], s_vs[r]), qop, acc,
+        consume_bits<D, P, FP8>(buf[r], m, tree_scale<FP8>(p.scale_log2, s_ks[r], s_vs[r]), qop, acc,
                                 m_run, l_run);
         if (++u >= steps) goto done;
       }
@@ -223,7 +214,7 @@ done:
     for (int w = 1; w < kSegWaves; ++w) M = fmaxf(M, s_ml[w][h].x);
 #pragma unroll
     for (int w = 0; w < kSegWaves; ++w) {
-      if (w >= n_steps) break;  // uniform: waves past the pages hold nothing
+      if (w >= n) break;  // uniform: waves past the pages hold nothing
       const float2 ml = s_ml[w][h];
       const float f = ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M);
       S += f * ml.y;
@@ -274,23 +265,15 @@ __global__ __launch_bounds__(256) void window_validate_kernel(ValidateParams p, 
   }
 }
 
-template <int D, int P, bool FP8>
-static const void* window_fn(int64_t grid) {
-  if constexpr (P == 16 && (FP8 || D == 64))
-    if (grid <= 512) return (const void*)&window_kernel<D, P, FP8, 32>;
-  return (const void*)&window_kernel<D, P, FP8, P>;
+template <int D, int P>
+static const void* window_fn(bool fp8) {
+  return fp8 ? (const void*)&window_kernel<D, P, true> : (const void*)&window_kernel<D, P, false>;
 }
 
 hipError_t launch_window(const WindowParams& p, bool fp8, hipStream_t s) {
-  const int64_t grid = (int64_t)p.num_seqs * p.num_kv_heads * p.chunks;
-  const void* fn;
-  if (p.head_dim == 128)
-    fn = p.page_size == 16
-             ? (fp8 ? window_fn<128, 16, true>(grid) : window_fn<128, 16, false>(grid))
-             : (fp8 ? window_fn<128, 32, true>(grid) : window_fn<128, 32, false>(grid));
-  else
-    fn = p.page_size == 16 ? (fp8 ? window_fn<64, 16, true>(grid) : window_fn<64, 16, false>(grid))
-                           : (fp8 ? window_fn<64, 32, true>(grid) : window_fn<64, 32, false>(grid));
+  const void* fn = p.head_dim == 128
+                       ? (p.page_size == 16 ? window_fn<128, 16>(fp8) : window_fn<128, 32>(fp8))
+                       : (p.page_size == 16 ? window_fn<64, 16>(fp8) : window_fn<64, 32>(fp8));
   WindowParams arg = p;
   void* args[] = {(void*)&arg};
   return hipLaunchKernel(fn, dim3((unsigned)(p.num_seqs * p.num_kv_heads), (unsigned)p.chunks),

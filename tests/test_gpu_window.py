@@ -57,7 +57,7 @@ def test_windows(dt, P, d, window, sinks):
 @pytest.mark.parametrize("dt", [0, 1])
 @pytest.mark.parametrize("G", [1, 7, 16])
 def test_groups_and_many_segments(dt, G):
-    """More (sequence, KV head) segments than 512: page by page instead of in pairs."""
+    """More (sequence, KV head) segments than workgroups fit the chip at once."""
     rng = np.random.default_rng(G)
     _case(rng.integers(0, 200, 300), 50, 5, 2, G, 64, 16, dt, seed=G)
 
@@ -87,7 +87,7 @@ def test_window_past_every_row_is_the_plain_decode():
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n", [1, 150])
 def test_odd_scales(d, P, n):
-    """n = 150: more segments than the steps over two pages take."""
+    """n = 150: many segments."""
     c = Cache([300, 100, 90, 211, 64, 50, 33] * n, 4, d, P, 1, seed=d + P)
     odd_scales(c)
     q = _q(7 * n, 8, d, P)

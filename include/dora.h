@@ -336,7 +336,9 @@ dora_status dora_kv_append(const dora_decode_desc* desc, const void* k_new, cons
  * run of a prompt.  With n = counts[b] (num_tokens without counts) and L =
  * seq_lens[b], which counts them, token i < n is row path[b][i] (row i without path) of
  * k_new[b] and v_new[b] and goes to position L - n + i.  The pages and scales end up as
- * after n calls of dora_kv_append, one token each in that order, bit for bit.
+ * after n calls of dora_kv_append, one token each in that order, bit for bit (only the sign
+ * of a NaN code of a page whose scale is NaN is open).  As there, the pages of one call must
+ * belong to distinct sequences; a page's other slots may be read and written back.
  *   num_tokens   T in [1, DORA_PATH_MAX_TOKENS], rows of k_new and v_new per sequence
  *   k_new, v_new device bf16 [B][T][Hkv][d], 16-byte aligned
  *   path         device int32 [B][T] or NULL; entries i >= n are not read; an index

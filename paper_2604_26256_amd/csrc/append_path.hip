@@ -10,12 +10,15 @@
 // 256 results of all of them together are kept in a table per growth, and each code
 // (an old one, or a new token's) is read, mapped and written once.
 //
-// Bound: bf16 by memory (24 runs of 300 to 700 tokens, 8 KV heads of 128 dims: 101 MB in
-// 22 us, 4.6 TB/s).  fp8 by the chain length -> page id -> scale and tokens -> scale's
-// course -> tables -> codes, each step a trip to memory or a barrier, and by the encoding:
-// 37 instructions a value through the division, whose ties sent most waves the long way
-// round a cheaper test, 17 with path_codes8 (the same runs in fp8 55 -> 30 us, 76 MB;
-// 1,024 paths of up to 16 tokens 65 -> 34 us).
+// Bound by memory, and by more of it than the tokens: a token's V is one element of every
+// head-dim row, so a page's V goes through whole whatever is new in it, and fp8 codes under
+// a growing scale are read and written again.  1,024 paths of up to 16 tokens (8 KV heads of
+// 128 dims): fp8 34 us for 133 MB that way (54 MB of tokens and codes alone), bf16 35 us; 24 runs
+// of 300 to 700 tokens bf16 22 us (101 MB, 4.6 TB/s), fp8 30 us (76 MB).  fp8 also by the
+// chain length -> page id -> scale and tokens -> scale's course -> tables -> codes, each
+// step a trip to memory or a barrier, and by the encoding: 37 instructions a value through
+// the division (whose ties sent most waves the long way round a cheaper test), 17 with
+// path_codes8 (the same calls 65 -> 34 and 55 -> 30 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

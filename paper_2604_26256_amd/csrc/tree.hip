@@ -14,7 +14,8 @@ namespace dora {
 constexpr int kTreeTiles = kTreeWaves;  // of a column block, at most
 // Pages whose ids (and fp8 scales) a workgroup holds in LDS at a time.
 constexpr int kTreeWindow = 512;
-// What a segment costs besides its steps (lengths, page ids, queries, the rows), in steps.
+// What a segment costs besides its steps (lengths, page ids, queries, the rows), in steps; 256
+// fp8 rows of 2,048 tokens at the median, 8 nodes: 539 us against 633 at 0.
 constexpr int kTreeWideCost = 4;
 
 // Row of a 32-token tile that holds token t, and the other way round (bits 2 and 3
@@ -38,8 +39,17 @@ __device__ __forceinline__ int tree_v_at(int row, int piece) {
 // A workgroup takes an equal, contiguous range of the batch's (sequence, KV head, column
 // block, step) list, as the plain decode's wavefronts do, or, where p.whole, one
 // (sequence, KV head, column block).
-//   A step's pages go HBM -> registers (two steps in flight) -> LDS, fp8 widened to bf16 on
-// the way, so that the four waves share one read and one conversion.
+//   A step's pages go HBM -> registers (two steps in flight; teams of two waves, whose shares
+// are twice as large, one: 122 us against 139 for the bf16 rows below) -> LDS, fp8 widened to bf16
+// on the way, so that the four waves share one read and one conversion.
+//   Bound by no one unit: with two waves a SIMD, the matrix pipe is busy for 41% of the cycles,
+// the vector ALU for 59% (16 of its 80 instructions a step are exponentials of 16 cycles), LDS
+// for 60%.  256 fp8 rows of 4,096 tokens at the median, 16 nodes, 64/8 heads of 128 dims (128
+// columns): 3.3 GB and 0.80 TFLOP in 1,040 us, 0.77 PFLOP/s (a large bf16 product 1.34).  64
+// bf16 rows of 2,048 at the median, up to 8 nodes, 28/4 heads (56 columns): 0.50 GB in 122 us.
+// Two tiles a wave without LDS for K and V (981 us for rows of 6,000 instead of 1,010, 1,440 for
+// rows of 500 instead of 960), a third workgroup per CU (bf16 145 -> 178 us) and the next step's
+// scores beside this one's weights (1,035 -> 1,107) do not pay.
 template <int D, int P, bool FP8, int NT>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) {
   constexpr int SP = kTreeWaves / NT, TT = 64 * NT, PAIR = 32 / P;

@@ -1,5 +1,8 @@
 // Tree attention for at most 32 columns (nodes x group) per KV head, a tile: the waves of a
 // workgroup take its steps in turn, and load them straight from HBM into matrix operands.
+// Bound by memory: 64 bf16 rows of 2,048 tokens at the median, 4 nodes, 28/4 heads of 128 dims:
+// 0.48 GB in 92 us with the join, 5.2 TB/s (through LDS, as tree.hip: 114); 256 fp8 rows, 64/8
+// heads, 2.0 GB in 369 us, 5.3 TB/s (431).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -7,7 +10,8 @@
 
 namespace dora {
 
-// What a segment costs besides its stages (lengths, page ids, queries, the merge), in stages.
+// What a segment costs besides its stages (lengths, page ids, queries, the merge), in stages: the
+// bf16 rows above 92 us against 105 at 0.
 constexpr int kTreeNarrowCost = 2;
 
 // Lane (row of K's tile or of V's, half h) and the 32 tokens of a step.  Register 8s + 4j +

@@ -253,7 +253,7 @@ dora_status dora_decode_attn_grouped(const dora_decode_desc* desc, const void* q
  * cache (a rejected draft leaves no trace in the pages or their scales); store what
  * is accepted with dora_kv_append_path.
  *   desc         as for dora_decode_attn; seq_lens counts the cached tokens only;
- *                num_waves (0 = library default) is rounded up to workgroups of 4,
+ *                num_waves (0 = library default) is rounded up to workgroups of 2 or 4,
  *                min_range_pages is not used
  *   num_nodes    T in [1, 64]
  *   q, out       device bf16 [B][T][Hq][d]

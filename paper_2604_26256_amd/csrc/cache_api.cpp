@@ -76,12 +76,15 @@ void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
   int64_t seqs = INT32_MAX / (steps * d.num_kv_heads * t->blocks);
   if (seqs > kTreeMaxSeqs) seqs = kTreeMaxSeqs;
   t->seqs = (int)(seqs < d.num_seqs ? seqs : d.num_seqs);
-  // Two workgroups a CU, but one where a wave holds two bf16 steps of 128 dims in registers (92 us
-  // against 123 with half the registers).
-  const bool large = t->tiles < 2 && d.head_dim == 128 && d.kv_dtype == DORA_KV_BF16;
-  const int64_t slots = (int64_t)compute_units() * (large ? 1 : 2);
+  // Workgroups a CU.  One tile: two, but one where a wave holds two bf16 steps of 128 dims in
+  // registers (92 us against 123 with half the registers).  Two tiles, of two waves: three (the 64
+  // fp8 columns of 256 rows 500 us, 588 with two, 520 with four; bf16's LDS has no room for four).
+  const bool large = d.head_dim == 128 && d.kv_dtype == DORA_KV_BF16;
+  const int waves = t->tiles == 2 ? 2 : kTreeWaves;  // of a workgroup
+  const int per_cu = t->tiles < 2 ? (large ? 1 : 2) : t->tiles == 2 ? 3 : 2;
+  const int64_t slots = (int64_t)compute_units() * per_cu;
   const int64_t most = (int64_t)t->seqs * d.num_kv_heads * t->blocks * steps;
-  t->workgroups = d.num_waves > 0 ? ((int64_t)d.num_waves + kTreeWaves - 1) / kTreeWaves
+  t->workgroups = d.num_waves > 0 ? ((int64_t)d.num_waves + waves - 1) / waves
                   : slots < most ? slots : most;
   if (t->workgroups < 1) t->workgroups = 1;
   size_t off = kWsHeaderBytes;
@@ -95,12 +98,17 @@ void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
 }
 
 // Whether a launch takes a workgroup per (sequence, KV head, column block), uncut: where no row
-// is longer than 2,048 tokens.  Against equal ranges and their join (8 KV heads of 128 dims, fp8):
-// 128 rows of 400 tokens at the median, up to 2,048, 4 nodes, 43 us for 53; 256 rows of up to
-// 1,024 (4 heads, bf16, 8 nodes) 66 for 73; 8 of 1,024 (2 heads of 64, bf16) 10.2 for 12.5; but 4
-// full rows of 2,048 46 for 42, and of 4,096 (8 rows, 2 heads of 64) 23 for 17.
-bool tree_whole(const dora_decode_desc& d) {
-  return d.num_waves <= 0 && (int64_t)d.block_table_stride * d.page_size <= 2048;
+// is longer than 2,048 tokens and, with more than one tile (whose workgroups take all of a row's
+// steps one by one), the workgroups fill the chip or no row passes 512.  Against equal ranges and
+// their join: one tile, 128 fp8 rows of 400 tokens at the median, 8 heads of 128, 43 us for 53, 8 bf16 rows
+// of 1,024, 2 heads of 64, 10.2 for 12.5, of 4,096, 23 for 17; two tiles, 256 bf16 rows of up to
+// 1,024, 4 heads, 60 for 67, 64 of 2,048, 62 for 76, but 4 fp8 rows of 1,024, 8 heads, 30 for 25, of
+// 2,048, 52 for 31.
+bool tree_whole(const dora_decode_desc& d, const TreeLayout& t, int seqs) {
+  const int64_t tokens = (int64_t)d.block_table_stride * d.page_size;
+  const int64_t groups = (int64_t)seqs * d.num_kv_heads * t.blocks;
+  return d.num_waves <= 0 &&
+         (tokens <= 512 || (tokens <= 2048 && (t.tiles < 2 || groups >= compute_units())));
 }
 
 // ---------------------------------------------------------------------------
@@ -221,7 +229,7 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
     p.group = d.num_q_heads / d.num_kv_heads;
     p.stride = d.block_table_stride;
     p.blocks = t.blocks;
-    p.whole = tree_whole(d) ? 1 : 0;
+    p.whole = tree_whole(d, t, p.num_seqs) ? 1 : 0;
     p.page_bytes = page_bytes_of(d);
     p.scale_log2 = scale_log2_of(d);
     const int64_t grid =

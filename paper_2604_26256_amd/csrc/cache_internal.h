@@ -12,13 +12,12 @@
 namespace dora {
 
 // Tree attention.
-constexpr int kTreeWaves = 4;        // waves of a workgroup
+constexpr int kTreeWaves = 4;        // waves of a workgroup (with two tiles: two)
 constexpr int kTreeMaxSeqs = 2048;   // sequences of a launch: their stage prefix lives in LDS
 
-// Tiles of 32 columns (a node's query heads, node by node) that a workgroup's team of waves
-// holds, for `columns` = nodes x group.  28 columns in one tile 92 us, in two 114; 56 in two tiles
-// 122, in four 130 (bf16; fp8, 32 and 64 columns: 371 and 431, 539 and 621; the rows are at the
-// kernels).
+// Tiles of 32 columns (a node's query heads, node by node) of a workgroup, for `columns` =
+// nodes x group.  28 columns in one tile 92 us, through LDS in two 114; 56 in two tiles 122, in four
+// 130 (bf16; fp8, 32 and 64 columns: 371 and 431, 539 and 621; the rows are at the kernels).
 inline int tree_tiles(int64_t columns) { return columns <= 32 ? 1 : columns <= 64 ? 2 : 4; }
 
 struct TreeParams {

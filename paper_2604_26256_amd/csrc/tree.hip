@@ -1,8 +1,8 @@
 // Decode attention for a tree of drafted tokens per sequence, over the paged cache and the
 // drafts' own keys and values.  All nodes of a sequence see its whole cache, so every
 // cached byte is applied to the C = nodes x group columns of its KV head; among the drafts
-// a column sees what its node's mask says.  This file: more than 64 columns, in blocks of
-// 128, a tile of 32 for each of a workgroup's four waves (fewer: tree_narrow.hip), and the
+// a column sees what its node's mask says.  This file: more than 32 columns, in blocks of 64 or
+// 128, a tile of 32 for each of a workgroup's waves (fewer: tree_narrow.hip), and the
 // join of cut segments.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -11,64 +11,60 @@
 
 namespace dora {
 
-constexpr int kTreeTiles = kTreeWaves;  // of a column block, at most
 // Pages whose ids (and fp8 scales) a workgroup holds in LDS at a time.
 constexpr int kTreeWindow = 512;
 // What a segment costs besides its steps (lengths, page ids, queries, the rows), in steps; 256
-// fp8 rows of 2,048 tokens at the median, 8 nodes: 539 us against 633 at 0.
-constexpr int kTreeWideCost = 4;
+// fp8 rows of 2,048 tokens at the median, 8 nodes: 492 us, 510 at 8, 530 at 4.
+constexpr int kTreeWideCost = 12;
 
-// Row of a 32-token tile that holds token t, and the other way round (bits 2 and 3
-// change places): the rows of a lane's accumulator, 16s + 8j + 4h + i, then are the tokens
-// 16s + 8h + 4j + i, the 8 consecutive tokens of k-step s that this lane supplies to the
-// second product.
-__device__ __forceinline__ int tree_row(int t) {
-  return (t & 0x13) | ((t & 4) << 1) | ((t & 8) >> 1);
-}
-// Registers of half h whose tokens are among `bits`.
-__device__ __forceinline__ uint32_t tree_registers(uint32_t bits, int h) {
-  return ((bits >> (8 * h)) & 0xFFu) | (((bits >> (16 + 8 * h)) & 0xFFu) << 8);
+// Waits until at most N of the wave's loads are under way.
+template <int N>
+__device__ __forceinline__ void tree_wait_loads() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);
 }
 
-// V's 16-byte pieces (8 tokens of a head-dim row, 4 pieces a row) change places with
-// the row so that 16 rows' pieces of one column lie in different banks.
-__device__ __forceinline__ int tree_v_at(int row, int piece) {
-  return row * 64 + ((piece ^ ((row >> 2) & 3)) << 4);
+// 64 pieces of 16 bytes, one a lane, into LDS in lane order, past the registers.
+__device__ __forceinline__ void tree_fetch(const uint8_t* from, uint8_t* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// A workgroup takes an equal, contiguous range of the batch's (sequence, KV head, column
-// block, step) list, as the plain decode's wavefronts do, or, where p.whole, one
-// (sequence, KV head, column block).
-//   A step's pages go HBM -> registers (two steps in flight; teams of two waves, whose shares
-// are twice as large, one: 122 us against 139 for the bf16 rows below) -> LDS, fp8 widened to bf16
-// on the way, so that the four waves share one read and one conversion.
-//   Bound by no one unit: with two waves a SIMD, the matrix pipe is busy for 41% of the cycles,
-// the vector ALU for 59% (16 of its 80 instructions a step are exponentials of 16 cycles), LDS
-// for 60%.  256 fp8 rows of 4,096 tokens at the median, 16 nodes, 64/8 heads of 128 dims (128
-// columns): 3.3 GB and 0.80 TFLOP in 1,040 us, 0.77 PFLOP/s (a large bf16 product 1.34).  64
-// bf16 rows of 2,048 at the median, up to 8 nodes, 28/4 heads (56 columns): 0.50 GB in 122 us.
-// Two tiles a wave without LDS for K and V (981 us for rows of 6,000 instead of 1,010, 1,440 for
-// rows of 500 instead of 960), a third workgroup per CU (bf16 145 -> 178 us) and the next step's
-// scores beside this one's weights (1,035 -> 1,107) do not pay.
+// A workgroup, a wave for each of its NT tiles of 32 columns, takes an equal, contiguous range of
+// the batch's (sequence, KV head, column block, step) list, as the plain decode's wavefronts do,
+// or, where p.whole, one (sequence, KV head, column block).
+//   A step's pages go from HBM straight into one of three LDS buffers, as they are, two steps ahead
+// of the one that all waves compute, with one barrier a step.  fp8 codes are widened by each wave
+// on the way into its products: four times the conversions of a kernel that does it on the way
+// into LDS, but half the LDS traffic, and no registers or instructions for the way in (that one:
+// 1,022 us for the 128-column fp8 rows below instead of 1,007, 156 for 139 in wide bf16 rows).  A
+// fourth buffer: 1,000 and 140 us, but 137 for 124 in the 56-column rows.
+//   Bound by no one unit: two waves a SIMD, whose vector and matrix instructions overlap in part.
+// 256 fp8 rows of 4,096 tokens at the median, 16 nodes, 64/8 heads of 128 dims (128 columns): 3.3 GB
+// and 0.80 TFLOP in 1,007 us, 0.79 PFLOP/s (a large bf16 product 1.34).  5 bf16 rows of 30,000, up to
+// 64 nodes, 32/8 heads: 139 us, 0.5 PFLOP/s.  64 bf16 rows of 2,048 at the median, up to 8 nodes,
+// 28/4 heads (56 columns): 0.50 GB in 124 us.  What does not pay: two tiles a wave straight from HBM
+// (rows of 6,000 981 us instead of 1,010, of 500 1,440 instead of 960), registers for three waves
+// a SIMD (they spill: wide rows 180), the next step's scores beside this one's weights.
 template <int D, int P, bool FP8, int NT>
-__global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) {
-  constexpr int SP = kTreeWaves / NT, TT = 64 * NT, PAIR = 32 / P;
+__global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
+  constexpr int TT = 64 * NT, PAIR = 32 / P, E = FP8 ? 1 : 2;
   constexpr int KS = D / 16, DB = D / 32, CB = 32 * NT;
-  constexpr int DEPTH = NT == 2 ? 1 : 2;
-  constexpr int TILE = P * D * (FP8 ? 1 : 2);      // bytes of one (page, KV head) tile
-  constexpr int NK = 32 * D * (FP8 ? 1 : 2) / 16;  // 16-byte pieces of a step's K (V: as many)
-  constexpr int PER = 2 * NK / TT;                 // pieces of a thread
-  constexpr int KB = 32 * D * 2;                   // LDS bytes of a step's K (V: as many)
+  constexpr int TILE = P * D * E;         // bytes of one (page, KV head) tile
+  constexpr int KB = PAIR * TILE;         // bytes of a step's K (V: as many)
+  constexpr int NK = KB / 16;             // ... in pieces of 16
+  constexpr int PER = 2 * NK / TT;        // pieces of a lane
+  constexpr int ROW = P * E / 16;         // pieces of a V row of a page
   static_assert(2 * NK % TT == 0 && NK / PAIR % 64 == 0, "a wave's 64 pieces are on one page");
-  __shared__ __align__(16) uint8_t s_kv[2][SP][2 * KB];
+  typedef TreeRegs<D, P, FP8> R;
+  typedef TreeTokens<P, FP8> Tok;
+  // (three variables: the compiler waits for what is loaded into the one that is read)
+  __shared__ __align__(16) uint8_t s_kv0[2 * KB], s_kv1[2 * KB], s_kv2[2 * KB];
   __shared__ int s_pid[kTreeWindow];
   __shared__ float s_ksc[FP8 ? kTreeWindow : 1], s_vsc[FP8 ? kTreeWindow : 1];
-  __shared__ float2 s_ml[kTreeWaves][32];
   extern __shared__ int s_pre[];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, tile = uni(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
-  const int team = wave / NT, tile = wave % NT, tt = tid - team * TT;
   const int Hkv = p.num_kv_heads, G = p.group;
 
   const int place = tree_place(p);
@@ -77,17 +73,25 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
   if (p.whole) {
     b = place / (Hkv * p.blocks);
   } else {
-    rg = tree_range<P, SP, CB, kTreeWideCost>(p, place, s_pre);
+    rg = tree_range<P, 1, CB, kTreeWideCost, NT>(p, place, s_pre);
     if (tid == 0) p.cuts[place] = make_int4(-1, 0, 0, 0);
     if (rg.x0 >= rg.x1) return;  // uniform
     b = rg.b;
   }
 
+  // In LDS a step's tiles are as in HBM, but that V's pieces of a row change places with the row,
+  // so that 16 rows' pieces of one column lie in different banks.  v_lane: what lane's piece of V
+  // is fetched from; k_at, v_turn: where the lane's operands are.
+  auto turn_of = [](int d) { return ROW == 4 ? (d >> 2) & 3 : ROW == 2 ? (d >> 3) & 1 : 0; };
+  const int v_lane = 16 * ((lane & ~(ROW - 1)) | ((lane & (ROW - 1)) ^ turn_of(lane / ROW)));
+  const int ktok_ = Tok::of_row(col), v_turn = turn_of(col);
+  const int k_at = (PAIR == 2 && ktok_ >= 16 ? TILE : 0) + (h * P + (ktok_ & (P - 1))) * 16;
+
   bool first_piece = true;
   int x = rg.x0;
   while (true) {
     // the piece: stages a .. z - 1 of (b, g, block)
-    const TreeSeq sq = tree_seq(p, b, P, SP, CB);
+    const TreeSeq sq = tree_seq(p, b, P, 1, CB);
     int g, blk, a, z, taken = 0;
     if (p.whole) {
       const int r = place - b * Hkv * p.blocks;
@@ -117,7 +121,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
     a = uni(a);
     z = uni(z);
     const int n_pages = uni(sq.pages), L = uni(sq.L), nodes = uni(sq.nodes);
-    const int cache_steps = uni(sq.cache_steps), cache_stages = uni(sq.cache_stages);
+    const int cache_stages = uni(sq.cache_stages);
 
     // query operand: this lane's column
     const int c = blk * CB + tile * 32 + col;
@@ -128,7 +132,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
     bf16x8 qop[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      qop[s] = *(const bf16x8*)(p.q + row * D + 16 * s + 8 * h);
+      qop[s] = *(const bf16x8*)(p.q + row * D +
+                                (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
       if (!mine) qop[s] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
     }
     const uint64_t live = nodes >= 64 ? ~0ull : (1ull << nodes) - 1;
@@ -142,25 +147,15 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
       for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
     float m_run = kNoMax, l_run = 0.f;
 
-    // The step in buffer `buf`; masked: the tokens of `bits` alone count.
-    auto consume = [&](int buf, bool masked, uint32_t bits, const TreeScale& s0, const TreeScale& s1) {
-      const uint8_t* kv = s_kv[buf][team];
-      const uint32_t own = masked ? tree_registers(bits, h) : 0xFFFFu;
-      tree_step<D, FP8, NT == 4>(
-          [&](int s) { return *(const bf16x8*)(kv + ((2 * s + h) * 32 + col) * 16); },
-          [&](int i, int s) { return *(const bf16x8*)(kv + KB + tree_v_at(32 * i + col, 2 * s + h)); },
-          s0, s1, masked, own, qop, acc, m_run, l_run);
-    };
-
     // Cached tokens, in windows of the pages whose ids fit the LDS array.
-    constexpr int WST = kTreeWindow / (PAIR * SP);  // stages of a window
+    constexpr int WST = kTreeWindow / PAIR;  // stages of a window
     const int c_end = z < cache_stages ? z : cache_stages;
     for (int w0 = a; w0 < c_end; w0 += WST) {
       const int n_st = c_end - w0 < WST ? c_end - w0 : WST;
-      const int j0 = w0 * SP * PAIR;
+      const int j0 = w0 * PAIR;
       const int n_win = n_pages - j0 < kTreeWindow ? n_pages - j0 : kTreeWindow;
       __syncthreads();  // the arrays and the buffers are free
-      for (int t = tid; t < n_win; t += 64 * kTreeWaves) {
+      for (int t = tid; t < n_win; t += TT) {
         const int pid = p.block_table[(int64_t)b * p.stride + j0 + t];
         s_pid[t] = pid;
         if constexpr (FP8) {
@@ -169,13 +164,13 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
         }
       }
       __syncthreads();
-      // Pages of the team's step of stage w0 + u (past the end the window's last).
+      // Pages of step w0 + u (past the end the window's last).
       auto page = [&](int u, int pg) {
-        const int at = (u * SP + team) * PAIR + pg;
+        const int at = u * PAIR + pg;
         return s_pid[at < n_win ? at : n_win - 1];
       };
-      auto load = [&](u32x4 (&r)[PER], int u, int v0, int v1) {
-        const int each = u < n_st ? 16 : 0;  // past the end the loads still issue, one line each
+      auto fetch = [&](uint8_t* kv, int u, int v0, int v1) {
+        const bool past = u >= n_st;  // past the end the loads still issue, one line each
         const int p0 = uni(v0), p1 = uni(v1);
         const int64_t base0 = (int64_t)p0 * p.page_bytes + (int64_t)g * TILE;
         const int64_t base1 = (int64_t)p1 * p.page_bytes + (int64_t)g * TILE;
@@ -187,57 +182,15 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
           const bool second = PAIR == 2 && i0 >= NK / 2;
           const int rem = (second ? i0 - NK / 2 : i0) * 16;
           const uint8_t* at = (is_v ? p.v_pages : p.k_pages) + (second ? base1 : base0) + rem;
-          r[k] = __builtin_nontemporal_load((const u32x4*)(at + lane * each));
+          tree_fetch(at + (past ? 0 : is_v ? v_lane : 16 * lane), kv + e0 * 16);
         }
       };
-      auto store = [&](const u32x4 (&r)[PER], int u, int buf) {
-        uint8_t* kv = s_kv[buf][team];
-        const int nv = L - ((w0 + u) * SP + team) * 32;  // tokens of the step that count
-#pragma unroll
-        for (int k = 0; k < PER; ++k) {
-          const int e = tt + k * TT;
-          const bool is_v = NK % TT == 0 ? TT * k >= NK : 64 * tile + TT * k >= NK;
-          const int idx = is_v ? e - NK : e;
-          const int pg = PAIR == 2 ? idx / (NK / 2) : 0, rem = PAIR == 2 ? idx - pg * (NK / 2) : idx;
-          u32x4 w = r[k];
-          if (!is_v) {
-            const int ch = rem / P, row_ = tree_row(pg * P + rem % P);
-            if constexpr (FP8) {
-              *(bf16x8*)(kv + ((2 * ch) * 32 + row_) * 16) = fp8x8_to_bf16(w[0], w[1]);
-              *(bf16x8*)(kv + ((2 * ch + 1) * 32 + row_) * 16) = fp8x8_to_bf16(w[2], w[3]);
-            } else {
-              *(u32x4*)(kv + (ch * 32 + row_) * 16) = w;
-            }
-          } else {
-            constexpr int TOK = FP8 ? 16 : 8, PR = P / TOK;  // tokens of a piece, pieces of a page's row
-            const int d = rem / PR, q = pg * PR + rem % PR;
-            if (nv < 32) {  // uniform: slots past the sequence hold anything
-              const int keep = nv - q * TOK;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int left = keep - i * (TOK / 4);
-                uint32_t m = 0;
-                if (left >= TOK / 4) m = ~0u;
-                else if (left > 0) m = (1u << (left * (FP8 ? 8 : 16))) - 1u;
-                w[i] &= m;
-              }
-            }
-            if constexpr (FP8) {
-              *(bf16x8*)(kv + KB + tree_v_at(d, 2 * q)) = fp8x8_to_bf16(w[0], w[1]);
-              *(bf16x8*)(kv + KB + tree_v_at(d, 2 * q + 1)) = fp8x8_to_bf16(w[2], w[3]);
-            } else {
-              *(u32x4*)(kv + KB + tree_v_at(d, q)) = w;
-            }
-          }
-        }
-      };
-      auto compute = [&](int u, int buf) {
-        const int step = (w0 + u) * SP + team;
-        if (!active || u >= n_st || step >= cache_steps) return;  // uniform in the wave
-        const int nv = L - step * 32;
+      auto compute = [&](const uint8_t* kv, int u) {
+        if (!active || u >= n_st) return;  // uniform in the wave
+        const int nv = L - (w0 + u) * 32;
         float ks0 = 1.f, ks1 = 1.f, vs0 = 1.f, vs1 = 1.f;
         if constexpr (FP8) {
-          const int at = (u * SP + team) * PAIR, at1 = PAIR == 2 && at + 1 < n_win ? at + 1 : at;
+          const int at = u * PAIR, at1 = PAIR == 2 && at + 1 < n_win ? at + 1 : at;
           ks0 = s_ksc[at];
           vs0 = s_vsc[at];
           ks1 = s_ksc[at1];
@@ -245,118 +198,108 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
         }
         const TreeScale s0 = tree_scale<FP8>(p.scale_log2, ks0, vs0);
         const TreeScale s1 = PAIR == 2 ? tree_scale<FP8>(p.scale_log2, ks1, vs1) : s0;
-        consume(buf, nv < 32, nv < 32 ? (1u << nv) - 1u : ~0u, s0, s1);
+        const bool masked = nv < 32;
+        const uint32_t own = masked ? Tok::registers((1u << nv) - 1u, h) : 0xFFFFu;
+        R r;
+#pragma unroll
+        for (int s = 0; s < R::NK; ++s) r.k[s] = *(const u32x4*)(kv + k_at + s * (2 * P * 16));
+        __builtin_amdgcn_sched_barrier(0);
+        tree_step<D, FP8>(
+            [&](int ks) { return tree_k(r, ks); },
+            [&] {  // V is read behind the scores, and waited for behind the softmax
+              typedef typename R::vraw_t V;
+#pragma unroll
+              for (int i = 0; i < DB; ++i) {
+                const uint8_t* row_ = kv + KB + (32 * i + col) * ROW * 16;
+                if constexpr (R::RUN16) {
+                  r.v[i] = *(const V*)(row_ + 16 * (h ^ v_turn));
+                } else {
+#pragma unroll
+                  for (int s = 0; s < 2; ++s) {
+                    if constexpr (FP8)
+                      r.v[2 * i + s] = *(const V*)(row_ + s * TILE + 8 * h);
+                    else if constexpr (PAIR == 2)
+                      r.v[2 * i + s] = *(const V*)(row_ + s * TILE + 16 * (h ^ v_turn));
+                    else
+                      r.v[2 * i + s] = *(const V*)(row_ + 16 * ((2 * s + h) ^ v_turn));
+                  }
+                }
+              }
+              __builtin_amdgcn_sched_barrier(0);
+              if (masked) tree_keep(r, own);  // slots past the sequence hold anything
+            },
+            [&](int i, int s) { return tree_v(r, i, s); }, s0, s1, masked, own, qop, acc, m_run, l_run);
       };
-      if constexpr (DEPTH == 1) {
-        // One stage in flight in registers, two in LDS: stage u + 1 goes from registers to
-        // LDS, and the loads of stage u + 2 are issued, before stage u is computed.
-        u32x4 r0[PER];
-        load(r0, 0, page(0, 0), page(0, 1));
-        int v0 = page(1, 0), v1 = page(1, 1);
-        store(r0, 0, 0);
-        load(r0, 1, v0, v1);
-        for (int u = 0; u < n_st; ++u) {
-          __syncthreads();
-          v0 = page(u + 2, 0);
-          v1 = page(u + 2, 1);
-          store(r0, u + 1, (u + 1) & 1);
-          load(r0, u + 2, v0, v1);
-          compute(u, u & 1);
-        }
-      } else {
-        u32x4 r0[PER], r1[PER];
-        int v0 = page(1, 0), v1 = page(1, 1);
-        load(r0, 0, page(0, 0), page(0, 1));
-        load(r1, 1, v0, v1);
-        v0 = page(2, 0);
-        v1 = page(2, 1);
-        store(r0, 0, 0);
-        load(r0, 2, v0, v1);
-        for (int u = 0; u < n_st; u += 2) {
-          __syncthreads();
-          v0 = page(u + 3, 0);
-          v1 = page(u + 3, 1);
-          store(r1, u + 1, 1);
-          load(r1, u + 3, v0, v1);
-          compute(u, 0);
-          // (no way out here: the compiler would wait at the top for what is loaded below)
-          __syncthreads();
-          v0 = page(u + 4, 0);
-          v1 = page(u + 4, 1);
-          store(r0, u + 2, 0);
-          load(r0, u + 4, v0, v1);
-          compute(u + 1, 1);
-        }
+      // Two stages on their way into LDS while a third is computed.  A wave's part of stage u has
+      // arrived when only the next stage's is under way, and all waves' when they have met;
+      // then they are done with stage u - 1 too, whose buffer takes stage u + 2.
+      int v0 = page(1, 0), v1 = page(1, 1);
+      fetch(s_kv0, 0, page(0, 0), page(0, 1));
+      fetch(s_kv1, 1, v0, v1);
+      v0 = page(2, 0);
+      v1 = page(2, 1);
+      auto turn = [&](uint8_t* now, uint8_t* next, int u) {
+        tree_wait_loads<PER>();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(next, u + 2, v0, v1);
+        v0 = page(u + 3, 0);
+        v1 = page(u + 3, 1);
+        compute(now, u);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      for (int u = 0; u < n_st; u += 3) {
+        turn(s_kv0, s_kv2, u);
+        turn(s_kv1, s_kv0, u + 1);
+        turn(s_kv2, s_kv1, u + 2);
       }
+      tree_wait_loads<0>();  // (the buffers are written otherwise below)
     }
 
-    // Drafts: rows of [node][d], V turned round on the way into LDS.
+    // Drafts (the last stages).  V is turned round on the way into LDS.
     for (int st = a > cache_stages ? a : cache_stages; st < z; ++st) {
-      const int t0 = ((st - cache_stages) * SP + team) * 32;  // first node of the team's step
+      const int t0 = (st - cache_stages) * 32;  // first node of the step
       __syncthreads();
-      uint8_t* kv = s_kv[0][team];
-      for (int e = tt; e < 32 * (D / 8); e += TT) {
+      uint8_t* vt = s_kv0;  // [d][32 nodes]
+      for (int e = tid; e < 32 * (D / 8); e += TT) {
         const int t = e / (D / 8), ch = e - t * (D / 8);
-        u32x4 kx{0u, 0u, 0u, 0u}, vx{0u, 0u, 0u, 0u};
-        if (t0 + t < nodes) {
-          const int64_t at = (((int64_t)b * p.num_nodes + t0 + t) * Hkv + g) * D + 8 * ch;
-          kx = *(const u32x4*)(p.k_draft + at);
-          vx = *(const u32x4*)(p.v_draft + at);
-        }
-        *(u32x4*)(kv + (ch * 32 + tree_row(t)) * 16) = kx;
+        u32x4 vx{0u, 0u, 0u, 0u};
+        if (t0 + t < nodes)
+          vx = *(const u32x4*)(p.v_draft + (((int64_t)b * p.num_nodes + t0 + t) * Hkv + g) * D + 8 * ch);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          *(uint16_t*)(kv + KB + tree_v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
+          *(uint16_t*)(vt + tree_v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
               (uint16_t)(vx[i >> 1] >> (16 * (i & 1)));
       }
       __syncthreads();
+      if (!active) continue;  // uniform in the wave
+      const int ktok = Tok::of_row(col);
+      const int t = t0 + ktok < nodes ? t0 + ktok : nodes - 1;  // a row past the nodes is masked
+      const uint16_t* kd = p.k_draft + (((int64_t)b * p.num_nodes + t) * Hkv + g) * D;
       const TreeScale one{p.scale_log2, 0.f, 1.f, 1.f};
-      if (active && t0 < nodes) consume(0, true, (uint32_t)(sees >> t0), one, one);
+      tree_step<D, FP8>(
+          [&](int s) {
+            return *(const bf16x8*)(kd + (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
+          },
+          [] {},
+          [&](int i, int s) {
+            return *(const bf16x8*)(vt + tree_v_at(32 * i + col, Tok::RUN16 ? 2 * h + s : 2 * s + h));
+          },
+          one, one, true, Tok::registers((uint32_t)(sees >> t0), h), qop, acc, m_run, l_run);
     }
 
-    // The piece's result: a tile's SP waves merged in LDS, each summing a share of the quads;
-    // then the rows, or one partial.
-    constexpr int QUADS = 4 * DB;
-    float S = sum_xor32(l_run), M = m_run;
-    f32x4* s_o = (f32x4*)&s_kv[0][0][0];  // [wave][quad][lane]
-    if constexpr (SP > 1) {
-      __syncthreads();  // the buffers are free
-      if (h == 0) s_ml[wave][col] = make_float2(m_run, S);
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < SP; ++w) M = fmaxf(M, s_ml[w * NT + tile][col].x);
-      S = 0.f;
-#pragma unroll
-      for (int w = 0; w < SP; ++w) {
-        const float2 ml = s_ml[w * NT + tile][col];
-        S += ml.y * (ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M));
-      }
-      const float f = m_run == M ? 1.f : __builtin_amdgcn_exp2f(m_run - M);
-#pragma unroll
-      for (int i = 0; i < DB; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          s_o[(wave * QUADS + 4 * i + j) * 64 + lane] =
-              f32x4{acc[i][4 * j] * f, acc[i][4 * j + 1] * f, acc[i][4 * j + 2] * f,
-                    acc[i][4 * j + 3] * f};
-      __syncthreads();
-    }
+    // The piece's result: rows, or one partial.
+    const float S = sum_xor32(l_run);
     const bool whole = a == 0 && z == sq.stages;
     const int64_t slot = 2 * (int64_t)place + (first_piece ? 0 : 1);
     const bool none = L == 0 && sees == 0;  // nothing to attend: zeros
     const float inv = none ? 0.f : 1.f / S;
 #pragma unroll
-    for (int k = 0; k < QUADS / SP; ++k) {
-      const int quad = team + SP * k, i = quad >> 2, j = quad & 3;
-      f32x4 o;
-      if constexpr (SP > 1) {
-        o = s_o[(tile * QUADS + quad) * 64 + lane];
-#pragma unroll
-        for (int w = 1; w < SP; ++w) o += s_o[((w * NT + tile) * QUADS + quad) * 64 + lane];
-      } else {
-        o = f32x4{acc[k >> 2][4 * (k & 3)], acc[k >> 2][4 * (k & 3) + 1], acc[k >> 2][4 * (k & 3) + 2],
-                  acc[k >> 2][4 * (k & 3) + 3]};
-      }
+    for (int quad = 0; quad < 4 * DB; ++quad) {
+      const int i = quad >> 2, j = quad & 3;
+      const f32x4 o{acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]};
       if (!whole) {
         if (active) ((f32x4*)(p.part_o + (slot * NT + tile) * 32 * D))[quad * 64 + lane] = o;
       } else if (mine) {
@@ -365,8 +308,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_kernel(TreeParams p) 
                    (__bf16)(o[3] * inv)};
       }
     }
-    if (!whole && active && team == 0 && h == 0)
-      p.part_ml[(slot * NT + tile) * 32 + col] = make_float2(M, S);
+    if (!whole && active && h == 0)
+      p.part_ml[(slot * NT + tile) * 32 + col] = make_float2(m_run, S);
     if (!whole && a == 0 && tid == 0)
       p.cuts[place] = make_int4(b, g * sq.blocks + blk,
                                      tree_pieces(rg, place, x + taken + (sq.stages - z) - 1), (int)slot);
@@ -440,8 +383,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeParams p) {
 
 template <int D, int P, bool FP8>
 static const void* wide_fn(int tiles) {
-  return tiles == 2 ? (const void*)&tree_kernel<D, P, FP8, 2>
-                    : (const void*)&tree_kernel<D, P, FP8, kTreeTiles>;
+  return tiles == 2 ? (const void*)&tree_kernel<D, P, FP8, 2> : (const void*)&tree_kernel<D, P, FP8, 4>;
 }
 
 hipError_t launch_tree_wide(const TreeParams& p, int D, int P, bool fp8, int tiles, int64_t grid,
@@ -456,7 +398,7 @@ hipError_t launch_tree_wide(const TreeParams& p, int D, int P, bool fp8, int til
   TreeParams arg = p;
   void* args[] = {(void*)&arg};
   const unsigned lds = p.whole ? 0 : (unsigned)(p.num_seqs + 1) * 4;
-  return hipLaunchKernel(fn, dim3((unsigned)grid), dim3(64 * kTreeWaves), args, lds, s);
+  return hipLaunchKernel(fn, dim3((unsigned)grid), dim3(64 * tiles), args, lds, s);
 }
 
 hipError_t launch_tree_combine(const TreeParams& p, int D, int tiles, int64_t grid, hipStream_t s) {
@@ -464,11 +406,11 @@ hipError_t launch_tree_combine(const TreeParams& p, int D, int tiles, int64_t gr
   if (D == 128)
     fn = tiles == 1   ? (const void*)&tree_combine_kernel<128, 1>
          : tiles == 2 ? (const void*)&tree_combine_kernel<128, 2>
-                      : (const void*)&tree_combine_kernel<128, kTreeTiles>;
+                      : (const void*)&tree_combine_kernel<128, 4>;
   else
     fn = tiles == 1   ? (const void*)&tree_combine_kernel<64, 1>
          : tiles == 2 ? (const void*)&tree_combine_kernel<64, 2>
-                      : (const void*)&tree_combine_kernel<64, kTreeTiles>;
+                      : (const void*)&tree_combine_kernel<64, 4>;
   TreeParams arg = p;
   void* args[] = {(void*)&arg};
   return hipLaunchKernel(fn, dim3((unsigned)grid, (unsigned)tiles, (unsigned)(D / 32)), dim3(256), args, 0, s);

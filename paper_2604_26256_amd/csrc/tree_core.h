@@ -60,12 +60,12 @@ struct TreeRange {
   int x0, x1, total, W, b;
 };
 
-template <int P, int SP, int CB, int COST>
+template <int P, int SP, int CB, int COST, int WAVES>
 __device__ __forceinline__ TreeRange tree_range(const TreeParams& p, int place, int* pre) {
-  __shared__ int s_wave[kTreeWaves];
+  __shared__ int s_wave[WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), B = p.num_seqs;
   int carry = 0;
-  for (int base = 0; base < B; base += 64 * kTreeWaves) {
+  for (int base = 0; base < B; base += 64 * WAVES) {
     int n = 0;
     if (base + tid < B) {
       const TreeSeq s = tree_seq(p, base + tid, P, SP, CB);
@@ -80,7 +80,7 @@ __device__ __forceinline__ TreeRange tree_range(const TreeParams& p, int place, 
     if (lane == 63) s_wave[wave] = incl;
     __syncthreads();
     int before = carry;
-    for (int w = 0; w < kTreeWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (w < wave) before += s_wave[w];
       carry += s_wave[w];
     }
@@ -146,49 +146,22 @@ __device__ __forceinline__ TreeScale tree_scale(float scale_log2, float k_scale,
 // its maximum.
 constexpr float kTreeMostWeight = 256.f;
 
-// A step over 32 tokens for a tile of 32 columns: S^T = K Q^T, softmax weights 2^(s - m) of
-// the log2 domain, O^T += V^T P^T.  Lane (column lane & 31, half h = lane >> 5) holds in its
-// registers 8s + e the scores of the 8 tokens that it supplies to k-step s of the second
-// product.  kf(ks): K operand of 16 head-dim values; vf(i, s): V operand of head-dim rows
-// 32i .. 32i + 31 and k-step s.  s0, s1: the scales of registers 0-7 and 8-15.  bits: the
-// registers that count for the lane's column, where some does not (masked, uniform: a
-// branch around the scores alone, as a second copy of the step would need registers for a
-// second set of accumulators).
+// Softmax weights of a step over 32 tokens for a tile of 32 columns: from the scores S^T = K Q^T,
+// the weights 2^(s - m) of the log2 domain, rounded to bf16 for the product O^T += V^T P^T.  Lane
+// (column lane & 31, half h = lane >> 5) holds in its registers 8s + e the scores of the 8
+// tokens that it supplies to k-step s of the second product.  s0, s1: the scales of
+// registers 0-7 and 8-15.  bits: the registers that count for the lane's column, where some
+// does not (masked, uniform: a branch around the scores alone, as a second copy of the step
+// would need registers for a second set of accumulators).
 //   m is a reference and not the running maximum: it moves only where the weights grow past
 // kTreeMostWeight, so that most steps neither look for their maximum nor rescale (96 of 175
-// vector instructions a step, the matrix products apart).  The weights are rounded to bf16
-// for the second product, and their sum is taken over the rounded ones: what the rounding
-// does to a row's largest weight then cancels.
-//   AHEAD: the operands come from LDS.  All of K's are read before the first product and
-// all of V's before the softmax, so that the reads' latency is waited for once, and the
-// second time behind the softmax (the compiler by itself reads two ahead).
-template <int D, bool FP8, bool AHEAD, typename KF, typename VF>
-__device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale s1, bool masked,
-                                          uint32_t bits, const bf16x8 (&qop)[D / 16],
-                                          f32x16 (&acc)[D / 32], float& m_run, float& l_run) {
-  constexpr int KS = D / 16, DB = D / 32;
-  f32x16 sc;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) sc[r] = 0.f;
-  bf16x8 op[AHEAD ? KS : 1];
-  if constexpr (AHEAD) {
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) op[ks] = kf(ks);
-    __builtin_amdgcn_sched_barrier(0);
-  }
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    if constexpr (AHEAD)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[ks], qop[ks], sc, 0, 0, 0);
-    else
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf(ks), qop[ks], sc, 0, 0, 0);
-  }
-  if constexpr (AHEAD) {
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int k = 0; k < KS; ++k) op[k] = vf(k >> 1, k & 1);
-    __builtin_amdgcn_sched_barrier(0);
-  }
+// vector instructions a step, the matrix products apart).  Their sum is taken over the
+// rounded weights: what the rounding does to a row's largest weight then cancels.
+template <int D, bool FP8>
+__device__ __forceinline__ void tree_weigh(f32x16& sc, TreeScale s0, TreeScale s1, bool masked,
+                                           uint32_t bits, f32x16 (&acc)[D / 32], float& m_run,
+                                           float& l_run, bf16x8 (&pb)[2]) {
+  constexpr int DB = D / 32;
   if (masked) {
     asm volatile("" : "+v"(bits));  // (else the 16 tests are made before the branch, every step)
 #pragma unroll
@@ -201,7 +174,6 @@ __device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale 
   }
   const float mul0 = s0.mul, mul1 = FP8 ? s1.mul : s0.mul;
   const float add0 = FP8 ? s0.add : 0.f, add1 = FP8 ? s1.add : 0.f;
-  bf16x8 pb[2];
   float sum[2];
   auto weigh = [&]() {
     const float b0 = add0 - m_run, b1 = add1 - m_run;
@@ -247,15 +219,121 @@ __device__ __forceinline__ void tree_step(KF kf, VF vf, TreeScale s0, TreeScale 
   } else {
     l_run += sum[0] + sum[1];
   }
+}
+
+// The whole step.  kf(ks): K operand of 16 head-dim values; vf(i, s): V operand of head-dim rows
+// 32i .. 32i + 31 and k-step s; scored(): called after the last use of K.
+template <int D, bool FP8, typename KF, typename SF, typename VF>
+__device__ __forceinline__ void tree_step(KF kf, SF scored, VF vf, TreeScale s0, TreeScale s1,
+                                          bool masked, uint32_t bits, const bf16x8 (&qop)[D / 16],
+                                          f32x16 (&acc)[D / 32], float& m_run, float& l_run) {
+  f32x16 sc;
 #pragma unroll
-  for (int i = 0; i < DB; ++i)
+  for (int r = 0; r < 16; ++r) sc[r] = 0.f;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if constexpr (AHEAD)
-        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[2 * i + s], pb[s], acc[i], 0, 0, 0);
-      else
-        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf(i, s), pb[s], acc[i], 0, 0, 0);
+  for (int ks = 0; ks < D / 16; ++ks)
+    sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf(ks), qop[ks], sc, 0, 0, 0);
+  scored();
+  bf16x8 pb[2];
+  tree_weigh<D, FP8>(sc, s0, s1, masked, bits, acc, m_run, l_run, pb);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf(i, s), pb[s], acc[i], 0, 0, 0);
+}
+
+// Lane (row of K's tile or of V's, half h) and the 32 tokens of a step.  Register 8s + 4j +
+// i of a lane is row 16s + 8j + 4h + i of the scores' tile; so that its 8 registers of
+// k-step s are 8 consecutive tokens, row r holds token row_token(r).  Where a V row of a
+// page is 32 bytes (fp8, 32 tokens), the lane's 16 tokens are consecutive: one 16-byte load.
+template <int P, bool FP8>
+struct TreeTokens {
+  static constexpr bool RUN16 = FP8 && P == 32;
+  static __device__ __forceinline__ int of_row(int r) {  // bits s j h i1 i0
+    const int s = (r >> 4) & 1, j = (r >> 3) & 1, h = (r >> 2) & 1;
+    return (RUN16 ? 16 * h + 8 * s : 16 * s + 8 * h) + 4 * j + (r & 3);
+  }
+  // Registers of half h whose tokens are among `bits`.
+  static __device__ __forceinline__ uint32_t registers(uint32_t bits, int h) {
+    if (RUN16) return (bits >> (16 * h)) & 0xFFFFu;
+    return ((bits >> (8 * h)) & 0xFFu) | (((bits >> (16 + 8 * h)) & 0xFFu) << 8);
+  }
+};
+
+// V's 16-byte pieces of 8 tokens in LDS (4 pieces a head-dim row) change places with the row,
+// so that 16 rows' pieces of one column lie in different banks.
+__device__ __forceinline__ int tree_v_at(int row, int piece) {
+  return row * 64 + ((piece ^ ((row >> 2) & 3)) << 4);
+}
+
+// A step's K and V as a lane loads them: K in 16-byte pieces, V in 16 (8: fp8, 16 tokens)
+// bytes per 32 head-dim rows and k-step (or both k-steps).
+template <int D, int P, bool FP8>
+struct TreeRegs {
+  static constexpr int NK = FP8 ? D / 32 : D / 16;
+  static constexpr bool RUN16 = TreeTokens<P, FP8>::RUN16;
+  static constexpr int NV = (D / 32) * (RUN16 ? 1 : 2);
+  typedef typename std::conditional<FP8 && !RUN16, u32x2, u32x4>::type vraw_t;
+  u32x4 k[NK];
+  vraw_t v[NV];
+};
+
+template <typename T>
+__device__ __forceinline__ T tree_load(const uint8_t* at) {
+  return __builtin_nontemporal_load((const T*)at);
+}
+
+// The V registers of a step whose tokens `own` alone count: the others, which may hold anything,
+// become zeros.
+template <int D, int P, bool FP8>
+__device__ __forceinline__ void tree_keep(TreeRegs<D, P, FP8>& r, uint32_t own) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    u32x4 keep;  // of the 8 tokens of k-step s: bf16 words, or (first two) fp8 words
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      keep[w] = 0;
+#pragma unroll
+      for (int e = 0; e < (FP8 ? 4 : 2); ++e) {
+        constexpr int BITS = FP8 ? 8 : 16;
+        const int tok = 8 * s + (FP8 ? 4 : 2) * w + e;
+        if ((!FP8 || w < 2) && ((own >> tok) & 1u)) keep[w] |= ((1u << BITS) - 1u) << (BITS * e);
+      }
     }
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      if constexpr (TreeRegs<D, P, FP8>::RUN16) {
+        r.v[i][2 * s] &= keep[0];
+        r.v[i][2 * s + 1] &= keep[1];
+      } else if constexpr (FP8) {
+        r.v[2 * i + s] &= u32x2{keep[0], keep[1]};
+      } else {
+        r.v[2 * i + s] &= keep;
+      }
+    }
+  }
+}
+
+// Operands out of a step's registers.
+template <int D, int P, bool FP8>
+__device__ __forceinline__ bf16x8 tree_k(const TreeRegs<D, P, FP8>& r, int ks) {
+  if constexpr (FP8) {
+    const u32x4& w = r.k[ks >> 1];
+    return (ks & 1) ? fp8x8_to_bf16(w[2], w[3]) : fp8x8_to_bf16(w[0], w[1]);
+  } else {
+    return __builtin_bit_cast(bf16x8, r.k[ks]);
+  }
+}
+
+template <int D, int P, bool FP8>
+__device__ __forceinline__ bf16x8 tree_v(const TreeRegs<D, P, FP8>& r, int i, int s) {
+  if constexpr (TreeRegs<D, P, FP8>::RUN16)
+    return s ? fp8x8_to_bf16(r.v[i][2], r.v[i][3]) : fp8x8_to_bf16(r.v[i][0], r.v[i][1]);
+  else if constexpr (FP8)
+    return fp8x8_to_bf16(r.v[2 * i + s][0], r.v[2 * i + s][1]);
+  else
+    return __builtin_bit_cast(bf16x8, r.v[2 * i + s]);
 }
 
 }  // namespace dora

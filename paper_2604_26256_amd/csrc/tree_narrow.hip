@@ -14,41 +14,6 @@ namespace dora {
 // bf16 rows above 92 us against 105 at 0.
 constexpr int kTreeNarrowCost = 2;
 
-// Lane (row of K's tile or of V's, half h) and the 32 tokens of a step.  Register 8s + 4j +
-// i of a lane is row 16s + 8j + 4h + i of the scores' tile; so that its 8 registers of
-// k-step s are 8 consecutive tokens, row r holds token row_token(r).  Where a V row of a
-// page is 32 bytes (fp8, 32 tokens), the lane's 16 tokens are consecutive: one 16-byte load.
-template <int P, bool FP8>
-struct TreeTokens {
-  static constexpr bool RUN16 = FP8 && P == 32;
-  static __device__ __forceinline__ int of_row(int r) {  // bits s j h i1 i0
-    const int s = (r >> 4) & 1, j = (r >> 3) & 1, h = (r >> 2) & 1;
-    return (RUN16 ? 16 * h + 8 * s : 16 * s + 8 * h) + 4 * j + (r & 3);
-  }
-  // Registers of half h whose tokens are among `bits`.
-  static __device__ __forceinline__ uint32_t registers(uint32_t bits, int h) {
-    if (RUN16) return (bits >> (16 * h)) & 0xFFFFu;
-    return ((bits >> (8 * h)) & 0xFFu) | (((bits >> (16 + 8 * h)) & 0xFFu) << 8);
-  }
-};
-
-// A step's K and V as a lane loads them: K in 16-byte pieces, V in 16 (8: fp8, 16 tokens)
-// bytes per 32 head-dim rows and k-step (or both k-steps).
-template <int D, int P, bool FP8>
-struct TreeRegs {
-  static constexpr int NK = FP8 ? D / 32 : D / 16;
-  static constexpr bool RUN16 = TreeTokens<P, FP8>::RUN16;
-  static constexpr int NV = (D / 32) * (RUN16 ? 1 : 2);
-  typedef typename std::conditional<FP8 && !RUN16, u32x2, u32x4>::type vraw_t;
-  u32x4 k[NK];
-  vraw_t v[NV];
-};
-
-template <typename T>
-__device__ __forceinline__ T tree_load(const uint8_t* at) {
-  return __builtin_nontemporal_load((const T*)at);
-}
-
 template <int D, int P, bool FP8>
 __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_narrow_kernel(TreeParams p) {
   constexpr int SP = kTreeWaves, PAIR = 32 / P;
@@ -71,7 +36,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
   if (p.whole) {
     b = place / Hkv;
   } else {
-    rg = tree_range<P, SP, 32, kTreeNarrowCost>(p, place, s_pre);
+    rg = tree_range<P, SP, 32, kTreeNarrowCost, SP>(p, place, s_pre);
     if (tid == 0) p.cuts[place] = make_int4(-1, 0, 0, 0);
     if (rg.x0 >= rg.x1) return;  // uniform
     b = rg.b;
@@ -203,50 +168,11 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
         uint32_t own = 0xFFFFu;
         if (masked) {  // slots past the sequence hold anything
           own = Tok::registers((1u << nv) - 1u, h);
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            u32x4 keep;  // of the 8 tokens of k-step s: bf16 words, or (first two) fp8 words
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              keep[w] = 0;
-#pragma unroll
-              for (int e = 0; e < (FP8 ? 4 : 2); ++e) {
-                constexpr int BITS = FP8 ? 8 : 16;
-                const int tok = 8 * s + (FP8 ? 4 : 2) * w + e;
-                if ((!FP8 || w < 2) && ((own >> tok) & 1u)) keep[w] |= ((1u << BITS) - 1u) << (BITS * e);
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-              if constexpr (R::RUN16) {
-                r.v[i][2 * s] &= keep[0];
-                r.v[i][2 * s + 1] &= keep[1];
-              } else if constexpr (FP8) {
-                r.v[2 * i + s] &= u32x2{keep[0], keep[1]};
-              } else {
-                r.v[2 * i + s] &= keep;
-              }
-            }
-          }
+          tree_keep(r, own);
         }
-        auto kf = [&](int ks) -> bf16x8 {
-          if constexpr (FP8) {
-            const u32x4& w = r.k[ks >> 1];
-            return (ks & 1) ? fp8x8_to_bf16(w[2], w[3]) : fp8x8_to_bf16(w[0], w[1]);
-          } else {
-            return __builtin_bit_cast(bf16x8, r.k[ks]);
-          }
-        };
-        auto vf = [&](int i, int s) -> bf16x8 {
-          if constexpr (R::RUN16) {
-            return s ? fp8x8_to_bf16(r.v[i][2], r.v[i][3]) : fp8x8_to_bf16(r.v[i][0], r.v[i][1]);
-          } else if constexpr (FP8) {
-            return fp8x8_to_bf16(r.v[2 * i + s][0], r.v[2 * i + s][1]);
-          } else {
-            return __builtin_bit_cast(bf16x8, r.v[2 * i + s]);
-          }
-        };
-        tree_step<D, FP8, false>(kf, vf, s0, s1, masked, own, qop, acc, m_run, l_run);
+        tree_step<D, FP8>([&](int ks) { return tree_k(r, ks); }, [] {},
+                          [&](int i, int s) { return tree_v(r, i, s); }, s0, s1, masked, own, qop, acc,
+                          m_run, l_run);
       };
       // The page ids are waited for here, once.
       asm volatile("" : "+v"(pid0), "+v"(pid1));
@@ -265,8 +191,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
       // the wave with the fewest cache steps first
       const int t0 = ((st - cache_stages) * SP + SP - 1 - wave) * 32;
       if (t0 >= nodes) continue;  // uniform in the wave
-      uint8_t* vt = (uint8_t*)&s_o[wave][0][0];  // [d][32 nodes], pieces of 8 displaced by row
-      auto v_at = [](int row_, int piece) { return row_ * 64 + ((piece ^ ((row_ >> 2) & 3)) << 4); };
+      uint8_t* vt = (uint8_t*)&s_o[wave][0][0];  // [d][32 nodes]
       for (int e = lane; e < 32 * (D / 8); e += 64) {
         const int t = e / (D / 8), ch = e - t * (D / 8);
         u32x4 vx{0u, 0u, 0u, 0u};
@@ -275,7 +200,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
                                (((int64_t)b * p.num_nodes + t0 + t) * Hkv + g) * D + 8 * ch);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          *(uint16_t*)(vt + v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
+          *(uint16_t*)(vt + tree_v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
               (uint16_t)(vx[i >> 1] >> (16 * (i & 1)));
       }
       const int t = t0 + ktok < nodes ? t0 + ktok : nodes - 1;  // a row past the nodes is masked
@@ -284,10 +209,10 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
         return *(const bf16x8*)(kd + (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
       };
       auto vf = [&](int i, int s) -> bf16x8 {
-        return *(const bf16x8*)(vt + v_at(32 * i + col, Tok::RUN16 ? 2 * h + s : 2 * s + h));
+        return *(const bf16x8*)(vt + tree_v_at(32 * i + col, Tok::RUN16 ? 2 * h + s : 2 * s + h));
       };
       const TreeScale one{p.scale_log2, 0.f, 1.f, 1.f};
-      tree_step<D, FP8, false>(kf, vf, one, one, true, Tok::registers((uint32_t)(sees >> t0), h), qop, acc,
+      tree_step<D, FP8>(kf, [] {}, vf, one, one, true, Tok::registers((uint32_t)(sees >> t0), h), qop, acc,
                         m_run, l_run);
     }
 

@@ -637,7 +637,7 @@ _thread = threading.local()  # workspaces of this thread's calls, by the call's 
 
 def _capturing(torch, stream):
     if stream is None:
-        return torch.cuda.is_current_stream_capturing()
+        return torch._C._cuda_isCurrentStreamCapturing()
     with torch.cuda.stream(stream):
         return torch.cuda.is_current_stream_capturing()
 
@@ -651,26 +651,34 @@ def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, workspace
     if torch._C._cuda_getDevice() != device.index:
         with torch.cuda.device(device):
             return _call_with_workspace(device, stream, where, args, bytes_fn, sizes, workspace)
-    need = int(getattr(_lib, bytes_fn)(args[0], *sizes))
-    if need == 0:  # invalid or unsupported: let the library name the reason
-        _call(device, stream, where, (*args, None, 0))
     if workspace is not None:
-        ptr, size = _dev_ptr(workspace, "workspace", (torch.uint8,)), workspace.numel()
+        ptr = _dev_ptr(workspace, "workspace", (torch.uint8,))
         if workspace.device != device:
             raise ValueError(f"workspace is on {workspace.device}, tensors on {device}")
+        return _call(device, stream, where, (*args, ptr, workspace.numel()))
+    handle = _stream_handle(stream, device)
+    capturing = _capturing(torch, stream)
+    cache = _thread.__dict__.setdefault(where, {})
+    workspace = None if capturing else cache.get((device.index, handle))
+    if workspace is not None:  # one that an earlier call needed: often large enough
+        st = getattr(_lib, where)(*args, workspace.data_ptr(), workspace.numel(), handle)
+        if st != DORA_ERR_WORKSPACE_TOO_SMALL:
+            return _check(st, where)
+    need = int(getattr(_lib, bytes_fn)(args[0], *sizes))
+    if need == 0:  # invalid or unsupported: let the library name the reason
+        return _call(device, stream, where, (*args, None, 0))
+    if capturing:
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
     else:
-        if _capturing(torch, stream):
-            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
-                workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        else:
-            cache = _thread.__dict__.setdefault(where, {})
-            workspace = _cached_workspace(cache, device, stream, need)
-        ptr, size = workspace.data_ptr(), need
-    _call(device, stream, where, (*args, ptr, size))
+        workspace = _cached_workspace(cache, device, stream, need)
+    _call(device, stream, where, (*args, workspace.data_ptr(), need))
 
 
 def _scale_specs(k_scales, v_scales, page_owner, num_pages):
-    """Specs of a pool's scales (fp8 pages: given; others: ignored) and owners."""
+    """Specs of a pool's scales (None but for fp8 pages) and owners."""
+    if k_scales is None and page_owner is None:
+        return ()
     torch = _torch()
     return [(k_scales, "k_scales", (torch.float32,), (num_pages,), 4),
             (v_scales, "v_scales", (torch.float32,), (num_pages,), 4),
@@ -810,10 +818,11 @@ def dora_kv_append_path(k_new, v_new, block_table, seq_lens, k_pages, v_pages, *
         (version_ids, "version_ids", i32, rows, 4),
         (k_pages, "k_pages", kv_types, None, 16),
         (v_pages, "v_pages", kv_types, None, 16),
-        *_scale_specs(k_scales, v_scales, page_owner, num_pages),
-        (dev_status, "dev_status", i32, None, 4)])
+        (dev_status, "dev_status", i32, None, 4),
+        *_scale_specs(k_scales, v_scales, page_owner, num_pages)])
+    scales = ptrs[10:12] if k_scales is not None else (None, None)
     _call(k_new.device, stream, "dora_kv_append_path",
-          (ctypes.byref(desc), T, *ptrs[:11], ptrs[12]))
+          (ctypes.byref(desc), T, *ptrs[:9], *scales, ptrs[9]))
 
 
 def dora_kv_page_copy(k_pages, v_pages, src_pages, dst_pages, *, num_kv_heads, page_size, head_dim,
@@ -838,12 +847,13 @@ def dora_kv_page_copy(k_pages, v_pages, src_pages, dst_pages, *, num_kv_heads, p
     ptrs = _marshal(k_pages.device, stream, [
         (k_pages, "k_pages", kv_types, None, 16),
         (v_pages, "v_pages", kv_types, None, 16),
-        *_scale_specs(k_scales, v_scales, None, num_pages)[:2],
         (src_pages if n else None, "src_pages", i32, None, 4),
         (dst_pages if n else None, "dst_pages", i32, None, 4),
-        (dev_status, "dev_status", i32, None, 4)])
+        (dev_status, "dev_status", i32, None, 4),
+        *_scale_specs(k_scales, v_scales, None, num_pages)])
+    scales = ptrs[5:7] if k_scales is not None else (None, None)
     _call(k_pages.device, stream, "dora_kv_page_copy",
-          (ctypes.byref(desc), *ptrs[:6], n, ptrs[6]))
+          (ctypes.byref(desc), *ptrs[:2], *scales, *ptrs[2:4], n, ptrs[4]))
 
 
 def plan_partition(workload, n_groups):

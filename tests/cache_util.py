@@ -83,8 +83,9 @@ class Cache:
             k, v = (x.view(torch.float8_e4m3fn) for x in (k, v))
         k, v = k.float().double().reshape(len(t), self.Hkv, self.d).numpy(), v.float().double().numpy()
         if self.dt == 1:
-            k = k * self.ks[ids].double().numpy()[:, None, None]
-            v = v * self.vs[ids].double().numpy()[:, None, None]
+            with np.errstate(invalid="ignore"):
+                k = k * self.ks[ids].double().numpy()[:, None, None]
+                v = v * self.vs[ids].double().numpy()[:, None, None]
         return k, v
 
 

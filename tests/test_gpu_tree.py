@@ -163,6 +163,37 @@ def test_far_pages():
     check(got, want, spread)
 
 
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("T,G", [(2, 8), (5, 8), (9, 8)])
+def test_rows_past_the_ids_held_at_a_time(dt, T, G):
+    """Around 512 pages of 16 tokens, whose ids a workgroup holds at once, and twice that, whole rows
+    in one range and cut."""
+    lens = [8191, 8192, 8193, 8224, 16400]
+    _case(lens, None, T, 1, G, 64, 16, dt, seed=T + dt, num_waves=4)
+    _case(lens, None, T, 1, G, 64, 16, dt, seed=T + dt)
+
+
+def test_workspaces_of_different_sizes_in_turn():
+    """Batches whose calls need less, more and less again than the workspace that is kept."""
+    D = lib()
+    runs = []
+    for n, (lens, T) in enumerate([([4000, 20], 4), ([3000, 2500, 4100], 40), ([2100], 9)]):
+        c = Cache(lens, 2, 64, 16, 0, seed=41 + n)
+        dev = c.gpu()
+        q, kd, vd = (x.cuda() for x in _drafts(len(lens), T, 2, 4, 64, [T] * len(lens), 43 + n))
+        mask = torch.from_numpy(random_trees(np.random.default_rng(n), [T] * len(lens), T).view(np.int64)).cuda()
+        a = (q, kd, vd, mask, dev["k"], dev["v"], dev["bt"], dev["lens"], None)
+        desc = D.make_decode_desc(num_seqs=len(lens), num_q_heads=8, num_kv_heads=2, head_dim=64, page_size=16,
+                                  block_table_stride=dev["bt"].shape[1], num_pages=c.num_pages)
+        ws = torch.empty(D.dora_decode_tree_workspace_bytes(desc, T), dtype=torch.uint8, device="cuda")
+        want = D.dora_decode_attn_tree(*a, torch.empty_like(q), workspace=ws, **dev["kw"])
+        runs.append((a, dev, want))
+    for n in (0, 1, 2, 1, 0):
+        a, dev, want = runs[n]
+        got = D.dora_decode_attn_tree(*a, torch.empty_like(want), **dev["kw"])
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16)), n
+
+
 def test_one_node_without_drafts_of_others_equals_the_decode():
     """A tree of one node over a cache, against the plain decode with that token appended."""
     D = lib()

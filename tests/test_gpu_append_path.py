@@ -181,6 +181,55 @@ def test_infinities_and_nan():
         _case([4, 0], [5, 4], 5, 2, 64, 16, dt, seed=7, values=odd)
 
 
+@pytest.mark.parametrize("dt", [0, 1])
+def test_graph_replays_and_streams(dt):
+    """A page copy and a path append, captured together and replayed with new tokens, against eager
+    calls, on the current stream and on another."""
+    D = lib()
+    g = torch.Generator().manual_seed(11 + dt)
+    B, T, Hkv, d, P = 9, 20, 2, 64, 16
+    start = [None if x is None else x.cuda() for x in _pool(5 * B, Hkv, d, P, dt, g)]
+    kn, vn = (torch.zeros(B, T, Hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    i32 = lambda x: torch.from_numpy(np.asarray(x, np.int32)).cuda()  # noqa: E731
+    perm = torch.randperm(5 * B, generator=g).to(torch.int32).numpy()
+    bt, src, dst = i32(perm[:4 * B].reshape(B, 4)), i32(perm[4 * B:]), i32(perm[:4 * B].reshape(B, 4)[:, 0])
+    before = torch.arange(B, dtype=torch.int32, device="cuda")
+    path = torch.randint(0, T, (B, T), generator=g, dtype=torch.int32).cuda()
+    counts = (torch.arange(B, dtype=torch.int32, device="cuda") * 3) % (T + 1)
+    lens = before + counts
+
+    def calls(pool, status, stream=None):
+        kw = dict(num_kv_heads=Hkv, page_size=P, kv_dtype=dt, k_scales=pool[2], v_scales=pool[3], dev_status=status, stream=stream)
+        D.dora_kv_page_copy(pool[0], pool[1], src, dst, head_dim=d, **kw)
+        D.dora_kv_append_path(kn, vn, bt, lens, pool[0], pool[1], path=path, counts=counts, **kw)
+
+    clone = lambda: [None if x is None else x.clone() for x in start]  # noqa: E731
+    captured, status = clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    calls(clone(), status)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(captured, status)
+    for step in range(4):
+        for x in (kn, vn):
+            x.copy_((torch.randn(x.shape, generator=g) * 2.0 ** (step - 1)).to(torch.bfloat16))
+        for x, y in zip(captured, start):
+            if x is not None:
+                x.copy_(y)
+        status.fill_(9)
+        graph.replay()
+        eager, other = clone(), clone()
+        calls(eager, None)
+        torch.cuda.synchronize()
+        calls(other, None, stream=torch.cuda.Stream())
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        for x, y, z in zip(captured, eager, other):
+            if x is not None:
+                dtype = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[x.element_size()]
+                assert torch.equal(x.view(dtype), y.view(dtype)) and torch.equal(z.view(dtype), y.view(dtype)), step
+
+
 def test_what_may_not_be_written_is_skipped_and_reported():
     """Bad page ids, lengths, counts and path entries: those pages (or sequences) stay as they
     were, the others are written, and the status says so."""

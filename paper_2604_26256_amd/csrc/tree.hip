@@ -33,22 +33,22 @@ __device__ __forceinline__ void tree_fetch(const uint8_t* from, uint8_t* to) {
 // the batch's (sequence, KV head, column block, step) list, as the plain decode's wavefronts do,
 // or, where p.whole, one (sequence, KV head, column block).
 //   A step's pages go from HBM straight into one of three LDS buffers, as they are, two steps ahead
-// of the one that all waves compute, with one barrier a step.  fp8 codes are widened by each wave
-// on the way into its products: four times the conversions of a kernel that does it on the way
-// into LDS, but half the LDS traffic, and no registers or instructions for the way in (that one:
-// 1,022 us for the 128-column fp8 rows below instead of 1,007, 156 for 139 in wide bf16 rows).  A
-// fourth buffer: 1,000 and 140 us, but 137 for 124 in the 56-column rows.
+// of the one that all waves compute, with one barrier a step.  V's fp8 codes (K's too, but for CODES) are
+// widened by each wave on the way into its products: four times the conversions of a kernel that
+// does it on the way into LDS, but half the LDS traffic, and no registers or instructions for the
+// way in (that one: 1,022 us for the 128-column fp8 rows below instead of 1,007, 156 for 139 in wide
+// bf16 rows).  A fourth buffer: 1,000 and 140 us, but 137 for 124 in the 56-column rows.
 //   Bound by no one unit: two waves a SIMD, whose vector and matrix instructions overlap in part.
 // 256 fp8 rows of 4,096 tokens at the median, 16 nodes, 64/8 heads of 128 dims (128 columns): 3.3 GB
-// and 0.80 TFLOP in 1,007 us, 0.79 PFLOP/s (a large bf16 product 1.34).  5 bf16 rows of 30,000, up to
+// and 0.80 TFLOP in 973 us with CODES, 0.82 PFLOP/s (a large bf16 product 1.34).  5 bf16 rows of 30,000, up to
 // 64 nodes, 32/8 heads: 139 us, 0.5 PFLOP/s.  64 bf16 rows of 2,048 at the median, up to 8 nodes,
 // 28/4 heads (56 columns): 0.50 GB in 124 us.  What does not pay: two tiles a wave straight from HBM
 // (rows of 6,000 981 us instead of 1,010, of 500 1,440 instead of 960), registers for three waves
 // a SIMD (they spill: wide rows 180), the next step's scores beside this one's weights.
-template <int D, int P, bool FP8, int NT>
+template <int D, int P, bool FP8, int NT, bool CODES>
 __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
   constexpr int TT = 64 * NT, PAIR = 32 / P, E = FP8 ? 1 : 2;
-  constexpr int KS = D / 16, DB = D / 32, CB = 32 * NT;
+  constexpr int DB = D / 32, CB = 32 * NT;
   constexpr int TILE = P * D * E;         // bytes of one (page, KV head) tile
   constexpr int KB = PAIR * TILE;         // bytes of a step's K (V: as many)
   constexpr int NK = KB / 16;             // ... in pieces of 16
@@ -123,19 +123,14 @@ __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
     const int n_pages = uni(sq.pages), L = uni(sq.L), nodes = uni(sq.nodes);
     const int cache_stages = uni(sq.cache_stages);
 
-    // query operand: this lane's column
+    // queries: this lane's column (one that is not there takes node 0's, for nothing)
     const int c = blk * CB + tile * 32 + col;
     const int node = c / G, head = c - node * G;
     const bool mine = node < nodes;
     const int64_t row = (((int64_t)b * p.num_nodes + (mine ? node : 0)) * p.num_q_heads +
                          (int64_t)g * G + (mine ? head : 0));
-    bf16x8 qop[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      qop[s] = *(const bf16x8*)(p.q + row * D +
-                                (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
-      if (!mine) qop[s] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-    }
+    TreeQuery<D, FP8, CODES> qop;
+    qop.load(p.q + row * D, h);
     const uint64_t live = nodes >= 64 ? ~0ull : (1ull << nodes) - 1;
     const uint64_t sees = mine ? p.tree_mask[(int64_t)b * p.num_nodes + node] & live : 0ull;
     const bool active = uni(blk * CB + tile * 32 < nodes * G);  // the wave's tile has columns
@@ -205,7 +200,7 @@ __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
         for (int s = 0; s < R::NK; ++s) r.k[s] = *(const u32x4*)(kv + k_at + s * (2 * P * 16));
         __builtin_amdgcn_sched_barrier(0);
         tree_step<D, FP8>(
-            [&](int ks) { return tree_k(r, ks); },
+            [&] { return tree_scores(r, qop); },
             [&] {  // V is read behind the scores, and waited for behind the softmax
               typedef typename R::vraw_t V;
 #pragma unroll
@@ -228,7 +223,7 @@ __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
               __builtin_amdgcn_sched_barrier(0);
               if (masked) tree_keep(r, own);  // slots past the sequence hold anything
             },
-            [&](int i, int s) { return tree_v(r, i, s); }, s0, s1, masked, own, qop, acc, m_run, l_run);
+            [&](int i, int s) { return tree_v(r, i, s); }, s0, s1, masked, own, acc, m_run, l_run);
       };
       // Two stages on their way into LDS while a third is computed.  A wave's part of stage u has
       // arrived when only the next stage's is under way, and all waves' when they have met;
@@ -280,14 +275,12 @@ __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
       const uint16_t* kd = p.k_draft + (((int64_t)b * p.num_nodes + t) * Hkv + g) * D;
       const TreeScale one{p.scale_log2, 0.f, 1.f, 1.f};
       tree_step<D, FP8>(
-          [&](int s) {
-            return *(const bf16x8*)(kd + (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
-          },
+          [&] { return tree_draft_scores(kd, p.q + row * D, qop, h); },
           [] {},
           [&](int i, int s) {
             return *(const bf16x8*)(vt + tree_v_at(32 * i + col, Tok::RUN16 ? 2 * h + s : 2 * s + h));
           },
-          one, one, true, Tok::registers((uint32_t)(sees >> t0), h), qop, acc, m_run, l_run);
+          one, one, true, Tok::registers((uint32_t)(sees >> t0), h), acc, m_run, l_run);
     }
 
     // The piece's result: rows, or one partial.
@@ -381,20 +374,27 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeParams p) {
              (__bf16)(acc[3] * inv)};
 }
 
+// CODES where vector instructions bound the waves (four tiles) and rows may be long enough for the
+// queries' codes, about 1 us a segment.  256 fp8 rows of 6,000 tokens, 128 columns: 943 us against
+// 1,003; of 1,500 tokens (800 rows) 843 against 850, of 700 level; in two tiles or whole rows of 500
+// slower by 4 to 5%.
 template <int D, int P, bool FP8>
-static const void* wide_fn(int tiles) {
-  return tiles == 2 ? (const void*)&tree_kernel<D, P, FP8, 2> : (const void*)&tree_kernel<D, P, FP8, 4>;
+static const void* wide_fn(int tiles, bool whole) {
+  if constexpr (FP8)
+    if (tiles == 4 && !whole) return (const void*)&tree_kernel<D, P, true, 4, true>;
+  return tiles == 2 ? (const void*)&tree_kernel<D, P, FP8, 2, false>
+                    : (const void*)&tree_kernel<D, P, FP8, 4, false>;
 }
 
 hipError_t launch_tree_wide(const TreeParams& p, int D, int P, bool fp8, int tiles, int64_t grid,
                             hipStream_t s) {
   const void* fn;
   if (D == 128)
-    fn = P == 16 ? (fp8 ? wide_fn<128, 16, true>(tiles) : wide_fn<128, 16, false>(tiles))
-                 : (fp8 ? wide_fn<128, 32, true>(tiles) : wide_fn<128, 32, false>(tiles));
+    fn = P == 16 ? (fp8 ? wide_fn<128, 16, true>(tiles, p.whole) : wide_fn<128, 16, false>(tiles, p.whole))
+                 : (fp8 ? wide_fn<128, 32, true>(tiles, p.whole) : wide_fn<128, 32, false>(tiles, p.whole));
   else
-    fn = P == 16 ? (fp8 ? wide_fn<64, 16, true>(tiles) : wide_fn<64, 16, false>(tiles))
-                 : (fp8 ? wide_fn<64, 32, true>(tiles) : wide_fn<64, 32, false>(tiles));
+    fn = P == 16 ? (fp8 ? wide_fn<64, 16, true>(tiles, p.whole) : wide_fn<64, 16, false>(tiles, p.whole))
+                 : (fp8 ? wide_fn<64, 32, true>(tiles, p.whole) : wide_fn<64, 32, false>(tiles, p.whole));
   TreeParams arg = p;
   void* args[] = {(void*)&arg};
   const unsigned lds = p.whole ? 0 : (unsigned)(p.num_seqs + 1) * 4;

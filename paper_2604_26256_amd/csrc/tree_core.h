@@ -12,6 +12,7 @@
 namespace dora {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // Smallest range of a workgroup, in stages.
 constexpr int kTreeMinRange = 2;
@@ -221,18 +222,13 @@ __device__ __forceinline__ void tree_weigh(f32x16& sc, TreeScale s0, TreeScale s
   }
 }
 
-// The whole step.  kf(ks): K operand of 16 head-dim values; vf(i, s): V operand of head-dim rows
-// 32i .. 32i + 31 and k-step s; scored(): called after the last use of K.
+// The whole step.  score(): the scores' tile, the last use of K; vf(i, s): V operand of head-dim
+// rows 32i .. 32i + 31 and k-step s; scored(): called between the two.
 template <int D, bool FP8, typename KF, typename SF, typename VF>
-__device__ __forceinline__ void tree_step(KF kf, SF scored, VF vf, TreeScale s0, TreeScale s1,
-                                          bool masked, uint32_t bits, const bf16x8 (&qop)[D / 16],
-                                          f32x16 (&acc)[D / 32], float& m_run, float& l_run) {
-  f32x16 sc;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) sc[r] = 0.f;
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
-    sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf(ks), qop[ks], sc, 0, 0, 0);
+__device__ __forceinline__ void tree_step(KF score, SF scored, VF vf, TreeScale s0, TreeScale s1,
+                                          bool masked, uint32_t bits, f32x16 (&acc)[D / 32],
+                                          float& m_run, float& l_run) {
+  f32x16 sc = score();
   scored();
   bf16x8 pb[2];
   tree_weigh<D, FP8>(sc, s0, s1, masked, bits, acc, m_run, l_run, pb);
@@ -315,17 +311,7 @@ __device__ __forceinline__ void tree_keep(TreeRegs<D, P, FP8>& r, uint32_t own) 
   }
 }
 
-// Operands out of a step's registers.
-template <int D, int P, bool FP8>
-__device__ __forceinline__ bf16x8 tree_k(const TreeRegs<D, P, FP8>& r, int ks) {
-  if constexpr (FP8) {
-    const u32x4& w = r.k[ks >> 1];
-    return (ks & 1) ? fp8x8_to_bf16(w[2], w[3]) : fp8x8_to_bf16(w[0], w[1]);
-  } else {
-    return __builtin_bit_cast(bf16x8, r.k[ks]);
-  }
-}
-
+// V's operands out of a step's registers.
 template <int D, int P, bool FP8>
 __device__ __forceinline__ bf16x8 tree_v(const TreeRegs<D, P, FP8>& r, int i, int s) {
   if constexpr (TreeRegs<D, P, FP8>::RUN16)
@@ -334,6 +320,140 @@ __device__ __forceinline__ bf16x8 tree_v(const TreeRegs<D, P, FP8>& r, int i, in
     return fp8x8_to_bf16(r.v[2 * i + s][0], r.v[2 * i + s][1]);
   else
     return __builtin_bit_cast(bf16x8, r.v[2 * i + s]);
+}
+
+// Head-dim offset of the 8 values that lane half h supplies to k-step s of the scores.  fp8: a
+// lane's 16-byte K piece is 16 values, its k-steps 2m and 2m + 1.
+template <bool FP8>
+__device__ __forceinline__ int tree_dim(int s, int h) {
+  return FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h;
+}
+
+// A lane's part of the queries, of column lane & 31: bf16 operands, or CODES.
+template <int D, bool FP8, bool CODES>
+struct TreeQuery {
+  bf16x8 op[D / 16];
+  __device__ __forceinline__ void load(const uint16_t* row, int h) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) op[s] = *(const bf16x8*)(row + tree_dim<FP8>(s, h));
+  }
+};
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// CODES: K's fp8 codes go into the products as they are, without the widening of each, so the
+// queries are codes too, two for each value: q = 2^e (hi + lo / 16), e per column and 64 dims.  A
+// bf16 value has 8 significant bits: hi is the nearest code, of 4, and what it leaves has 4 too, so
+// the sum is exact but where lo is subnormal, and there off by 2^-14 2^e, 2^-21 of the largest of
+// the 64 (an infinity or NaN makes all 64 NaN, as it makes the row).  Two fp8 products take the
+// matrix pipe as long as the bf16 one does.
+template <int D>
+struct TreeQuery<D, true, true> {
+  i32x8 hi[D / 64], lo[D / 64];
+  int scales;  // bytes: 2^e of hi[0], lo[0], hi[1], lo[1], biased by 127
+  __device__ __forceinline__ void load(const uint16_t* row, int h) {
+    scales = 0;
+#pragma unroll
+    for (int m = 0; m < D / 64; ++m) {
+      u32x4 w[4];  // the lane's K pieces 2m and 2m + 1
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[k] = *(const u32x4*)(row + tree_dim<true>(4 * m + k, h));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a = w[k][i] & 0x7FFFu, c = (w[k][i] >> 16) & 0x7FFFu;
+          top = top > a ? top : a;
+          top = top > c ? top : c;
+        }
+      }
+      const uint32_t there = (uint32_t)__shfl_xor((int)top, 32);  // the column's other values
+      top = top > there ? top : there;
+      // the largest becomes 128 to 255; be: its biased exponent, 14 to 255
+      int be = (int)(top >> 7);
+      be = be < 14 ? 14 : be;
+      const float down = __uint_as_float((uint32_t)(261 - be) << 23);  // 2^-e, e = be - 134
+      scales |= (int)((uint32_t)(be - 7) << (16 * m) | (uint32_t)(be - 11) << (16 * m + 8));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {  // 4 values each
+        uint32_t a = 0, c = 0;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const uint32_t v = w[k >> 1][2 * (k & 1) + p];
+          const float x = __uint_as_float(v << 16) * down, y = __uint_as_float(v & 0xFFFF0000u) * down;
+          if (p) {
+            a = __builtin_amdgcn_cvt_pk_fp8_f32(x, y, a, true);
+            c = __builtin_amdgcn_cvt_pk_fp8_f32((x - __builtin_amdgcn_cvt_f32_fp8(a, 2)) * 16.f,
+                                                (y - __builtin_amdgcn_cvt_f32_fp8(a, 3)) * 16.f, c, true);
+          } else {
+            a = __builtin_amdgcn_cvt_pk_fp8_f32(x, y, a, false);
+            c = __builtin_amdgcn_cvt_pk_fp8_f32((x - __builtin_amdgcn_cvt_f32_fp8(a, 0)) * 16.f,
+                                                (y - __builtin_amdgcn_cvt_f32_fp8(a, 1)) * 16.f, c, false);
+          }
+        }
+        hi[m][k] = top < 0x7F80u ? (int)a : 0x7F7F7F7F;
+        lo[m][k] = (int)c;
+      }
+    }
+  }
+};
+
+// Scores of a step's K for a tile of columns.
+template <int D, int P, bool FP8, bool CODES>
+__device__ __forceinline__ f32x16 tree_scores(const TreeRegs<D, P, FP8>& r,
+                                              const TreeQuery<D, FP8, CODES>& q) {
+  f32x16 sc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+  if constexpr (CODES) {
+    constexpr int ONE = 127;  // 2^0
+#pragma unroll
+    for (int m = 0; m < D / 64; ++m) {
+      const i32x8 k = __builtin_shufflevector(__builtin_bit_cast(i32x4, r.k[2 * m]),
+                                              __builtin_bit_cast(i32x4, r.k[2 * m + 1]), 0, 1, 2, 3, 4, 5,
+                                              6, 7);
+      if (m == 0) {  // (the byte of the scales is a constant)
+        sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.hi[m], sc, 0, 0, 0, ONE, 0, q.scales);
+        sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.lo[m], sc, 0, 0, 0, ONE, 1, q.scales);
+      } else {
+        sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.hi[m], sc, 0, 0, 0, ONE, 2, q.scales);
+        sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.lo[m], sc, 0, 0, 0, ONE, 3, q.scales);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      bf16x8 k;
+      if constexpr (FP8) {
+        const u32x4& w = r.k[ks >> 1];
+        k = (ks & 1) ? fp8x8_to_bf16(w[2], w[3]) : fp8x8_to_bf16(w[0], w[1]);
+      } else {
+        k = __builtin_bit_cast(bf16x8, r.k[ks]);
+      }
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q.op[ks], sc, 0, 0, 0);
+    }
+  }
+  return sc;
+}
+
+// Scores of 32 drafts: K row `key` of the lane, and for CODES the column's row of q, both bf16.
+template <int D, bool FP8, bool CODES>
+__device__ __forceinline__ f32x16 tree_draft_scores(const uint16_t* key, const uint16_t* row,
+                                                    const TreeQuery<D, FP8, CODES>& q, int h) {
+  f32x16 sc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const int at = tree_dim<FP8>(s, h);
+    bf16x8 op;
+    if constexpr (CODES)
+      op = *(const bf16x8*)(row + at);
+    else
+      op = q.op[s];
+    sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(key + at), op, sc, 0, 0, 0);
+  }
+  return sc;
 }
 
 }  // namespace dora

@@ -17,7 +17,7 @@ constexpr int kTreeNarrowCost = 2;
 template <int D, int P, bool FP8>
 __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_narrow_kernel(TreeParams p) {
   constexpr int SP = kTreeWaves, PAIR = 32 / P;
-  constexpr int KS = D / 16, DB = D / 32, E = FP8 ? 1 : 2;
+  constexpr int DB = D / 32, E = FP8 ? 1 : 2;
   constexpr int TILE = P * D * E;  // bytes of one (page, KV head) tile
   constexpr int QUADS = 4 * DB;    // accumulator quads of a tile
   typedef TreeRegs<D, P, FP8> R;
@@ -94,24 +94,16 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     };
     if (steps > 0) load_ids(0);
 
-    // query operand and mask: this lane's column.  fp8: a lane's 16-byte K piece is 16 head-dim
-    // values, its k-steps 2m and 2m + 1.
+    // queries and mask: this lane's column (one that is not there takes node 0's, for nothing)
     const int node = col / G, head = col - node * G;
     const bool mine = node < nodes;
     const int64_t row = (((int64_t)b * p.num_nodes + (mine ? node : 0)) * p.num_q_heads +
                          (int64_t)g * G + (mine ? head : 0));
-    bf16x8 qop[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-      qop[s] = *(const bf16x8*)(p.q + row * D +
-                                (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
+    TreeQuery<D, FP8, false> qop;
+    qop.load(p.q + row * D, h);
     uint64_t sees = p.tree_mask[(int64_t)b * p.num_nodes + (mine ? node : 0)];
     sees &= nodes >= 64 ? ~0ull : (1ull << nodes) - 1;
-    if (!mine) {
-      sees = 0;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) qop[s] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-    }
+    if (!mine) sees = 0;
 
     f32x16 acc[DB];
     float m_run = kNoMax, l_run = 0.f;
@@ -170,9 +162,9 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
           own = Tok::registers((1u << nv) - 1u, h);
           tree_keep(r, own);
         }
-        tree_step<D, FP8>([&](int ks) { return tree_k(r, ks); }, [] {},
-                          [&](int i, int s) { return tree_v(r, i, s); }, s0, s1, masked, own, qop, acc,
-                          m_run, l_run);
+        tree_step<D, FP8>([&] { return tree_scores(r, qop); }, [] {},
+                          [&](int i, int s) { return tree_v(r, i, s); }, s0, s1, masked, own, acc, m_run,
+                          l_run);
       };
       // The page ids are waited for here, once.
       asm volatile("" : "+v"(pid0), "+v"(pid1));
@@ -205,15 +197,12 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
       }
       const int t = t0 + ktok < nodes ? t0 + ktok : nodes - 1;  // a row past the nodes is masked
       const uint16_t* kd = p.k_draft + (((int64_t)b * p.num_nodes + t) * Hkv + g) * D;
-      auto kf = [&](int s) -> bf16x8 {
-        return *(const bf16x8*)(kd + (FP8 ? 16 * (2 * (s >> 1) + h) + 8 * (s & 1) : 16 * s + 8 * h));
-      };
       auto vf = [&](int i, int s) -> bf16x8 {
         return *(const bf16x8*)(vt + tree_v_at(32 * i + col, Tok::RUN16 ? 2 * h + s : 2 * s + h));
       };
       const TreeScale one{p.scale_log2, 0.f, 1.f, 1.f};
-      tree_step<D, FP8>(kf, [] {}, vf, one, one, true, Tok::registers((uint32_t)(sees >> t0), h), qop, acc,
-                        m_run, l_run);
+      tree_step<D, FP8>([&] { return tree_draft_scores(kd, p.q + row * D, qop, h); }, [] {}, vf, one, one,
+                        true, Tok::registers((uint32_t)(sees >> t0), h), acc, m_run, l_run);
     }
 
     // The piece's result: the waves' merged in LDS, each summing a share of the quads; then the

@@ -115,6 +115,30 @@ def test_odd_scales(d, P, T, G):
     check(_run(c, q, kd, vd, mask, ns, out), want, spread, "tree", roundings=2)
 
 
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("P", [16, 32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_of_any_magnitude(dt, P, d):
+    """Elements of 2^-14 to 4 of their row's scale, rows of zeros, of subnormals, of one large element,
+    and with an infinity or a NaN, which make the row NaN.  Scores: what the fp8 products leave of a
+    query is 2^-21 of its largest element (8), so 8 * 2^-21 * sum |k| (128 of 0.8) is below 2^-11, with
+    the softmax scale and log2(e) below 2^-13."""
+    T, G, lens = 16, 8, [2500, 3000, 100, 0]
+    c = Cache(lens, 1, d, P, dt, seed=d + P)
+    q, kd, vd = _drafts(4, T, 1, G, d, [T] * 4, 7)
+    g = torch.Generator().manual_seed(9)
+    q = (q.float() * 2.0 ** torch.randint(-14, 2, q.shape, generator=g)).clamp(-8, 8)
+    q[0, 1], q[0, 2] = 0.0, q[0, 2] * 2.0 ** -132
+    q[0, 3] *= 2.0 ** -9
+    q[0, 3, :, 5] = 8.0
+    q[1, 4, 3, 7], q[1, 5, 0, d - 1], q[2, 6, 1, 0] = float("inf"), -float("inf"), float("nan")
+    q = q.to(torch.bfloat16)
+    mask = random_trees(np.random.default_rng(3), [T] * 4, T)
+    out = torch.zeros(4, T, G, d, dtype=torch.bfloat16)
+    want, spread = tree_reference(c, q, kd, vd, mask, [T] * 4, out)
+    check(_run(c, q, kd, vd, mask, None, out), want, spread, "tree")
+
+
 def test_infinite_scores():
     """Keys of -inf: no weight; of all visible tokens: NaN, as the definition gives."""
     for lens in ([40, 600], [40, 30]):

@@ -119,11 +119,11 @@ __device__ __forceinline__ int tree_pieces(const TreeRange& r, int place, int la
 }
 
 // What the 8 accumulator registers of a page's tokens are scaled by.  fp8: the page's V
-// scale goes into the exponent, so that the largest weight of a column is 1 and its
-// rounding to bf16 exact (with the scaling between the weight and its rounding the results
-// were off by 0.0025 of their size against 64 bits, by 0.0022 without; 0.0017 is the
-// rounding of the result itself); the sum of the weights is over 2^add then.  A V scale that
-// has no such logarithm (0, negative, not finite, far from 1) stays a factor.
+// scale goes into the exponent, so that a weight is rounded once and the sum (over 2^add then)
+// takes the rounded ones: for a row's largest weight the rounding cancels (with the scaling
+// between the weight and its rounding the results were off by 0.0025 of their size against 64
+// bits, by 0.0022 without; 0.0017 is the rounding of the result itself).  A V scale that has
+// no such logarithm (0, negative, not finite, far from 1) stays a factor.
 struct TreeScale {
   float mul;   // scores
   float add;   // added to the scaled scores, log2 units

@@ -249,7 +249,8 @@ dora_status dora_decode_attn_grouped(const dora_decode_desc* desc, const void* q
  *   out[b][i][h] = softmax over all of them, applied to V_t and v_draft[b][j][g]
  * A node that sees nothing (L = 0 and no bit) gives 0; rows of nodes i >= n are left
  * as they were.  The mask is taken as it is: a node that attends itself has its own
- * bit set, and bits of nodes >= n count as 0.  The drafts' K and V are not in the
+ * bit set, and bits of nodes >= n count as 0.  What a draft holds, infinities and NaN
+ * too, reaches the nodes that attend it alone.  The drafts' K and V are not in the
  * cache (a rejected draft leaves no trace in the pages or their scales); store what
  * is accepted with dora_kv_append_path.
  *   desc         as for dora_decode_attn; seq_lens counts the cached tokens only;

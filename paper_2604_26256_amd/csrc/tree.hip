@@ -59,7 +59,7 @@ __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
   typedef TreeTokens<P, FP8> Tok;
   // (three variables: the compiler waits for what is loaded into the one that is read)
   __shared__ __align__(16) uint8_t s_kv0[2 * KB], s_kv1[2 * KB], s_kv2[2 * KB];
-  __shared__ int s_pid[kTreeWindow];
+  __shared__ int s_pid[kTreeWindow], s_odd[NT];
   __shared__ float s_ksc[FP8 ? kTreeWindow : 1], s_vsc[FP8 ? kTreeWindow : 1];
   extern __shared__ int s_pre[];
 
@@ -254,21 +254,16 @@ __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
     }
 
     // Drafts (the last stages).  V is turned round on the way into LDS.
+    int any_odd = 0;  // among V something is not finite
     for (int st = a > cache_stages ? a : cache_stages; st < z; ++st) {
       const int t0 = (st - cache_stages) * 32;  // first node of the step
       __syncthreads();
       uint8_t* vt = s_kv0;  // [d][32 nodes]
-      for (int e = tid; e < 32 * (D / 8); e += TT) {
-        const int t = e / (D / 8), ch = e - t * (D / 8);
-        u32x4 vx{0u, 0u, 0u, 0u};
-        if (t0 + t < nodes)
-          vx = *(const u32x4*)(p.v_draft + (((int64_t)b * p.num_nodes + t0 + t) * Hkv + g) * D + 8 * ch);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          *(uint16_t*)(vt + tree_v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
-              (uint16_t)(vx[i >> 1] >> (16 * (i & 1)));
-      }
+      const bool odd = tree_put_drafts<D, TT>(p, vt, b, g, t0, nodes, tid);
+      if (lane == 0) s_odd[tile] = odd;
       __syncthreads();
+#pragma unroll
+      for (int w = 0; w < NT; ++w) any_odd |= s_odd[w];  // (stored again behind the next step's first barrier)
       if (!active) continue;  // uniform in the wave
       const int ktok = Tok::of_row(col);
       const int t = t0 + ktok < nodes ? t0 + ktok : nodes - 1;  // a row past the nodes is masked
@@ -299,6 +294,18 @@ __global__ __launch_bounds__(64 * NT, 2) void tree_kernel(TreeParams p) {
         *(bf16x4*)(p.out + row * D + 32 * i + 8 * j + 4 * h) =
             bf16x4{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv),
                    (__bf16)(o[3] * inv)};
+      }
+    }
+    if (__builtin_expect(uni(any_odd) && active, 0)) {
+      // the piece's own drafts, one step's or both: another's may weigh nothing in this piece
+      const uint64_t own = (a > cache_stages ? ~0ull << 32 : ~0ull) & (z > cache_stages + 1 ? ~0ull : ~0u);
+      for (int quad = 0; quad < 4 * DB; ++quad) {
+        const int d0 = tree_quad_dim(quad, h);
+        const f32x4 add = tree_odd_values(p, D, b, g, sees & own, d0);
+        if (!whole)
+          tree_add_odd(&((f32x4*)(p.part_o + (slot * NT + tile) * 32 * D))[quad * 64 + lane], add);
+        else if (mine)
+          tree_add_odd((bf16x4*)(p.out + row * D + d0), add);
       }
     }
     if (!whole && active && h == 0)

@@ -13,6 +13,7 @@ namespace dora {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // Smallest range of a workgroup, in stages.
 constexpr int kTreeMinRange = 2;
@@ -454,6 +455,87 @@ __device__ __forceinline__ f32x16 tree_draft_scores(const uint16_t* key, const u
     sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(key + at), op, sc, 0, 0, 0);
   }
   return sc;
+}
+
+// Infinities and NaN in V of a draft belong to the nodes that attend it.  Among the operands of a
+// product they would reach all of a tile's columns, since 0 x inf is NaN: so the products take zeros in
+// their place, and where a piece has any (seldom) they are added to its results, once these are stored.
+
+// V of 32 drafts from t0 on into LDS ([d][32 drafts], turned round), by THREADS threads, this one's
+// part; whether a value in the wave's part is not finite (in the wave, uniform).
+template <int D, int THREADS>
+__device__ __forceinline__ bool tree_put_drafts(const TreeParams& p, uint8_t* vt, int b, int g, int t0,
+                                                int nodes, int thread) {
+  constexpr int PIECES = 32 * (D / 8) / THREADS;  // of a thread, 8 values each
+  constexpr int BATCH = PIECES < 2 ? 1 : 2;       // loaded together
+  static_assert(32 * (D / 8) % THREADS == 0 && PIECES % BATCH == 0, "whole batches");
+  bool odd = false;
+  while (true) {  // once, or twice where something is odd
+    u16x2 top{0, 0};  // the largest magnitude's bits
+#pragma unroll 1
+    for (int k = 0; k < PIECES; k += BATCH) {
+      u32x4 x[BATCH];
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int e = thread + THREADS * (k + j), t = e / (D / 8), ch = e - t * (D / 8);
+        x[j] = u32x4{0u, 0u, 0u, 0u};
+        if (t0 + t < nodes)
+          x[j] = *(const u32x4*)(p.v_draft + (((int64_t)b * p.num_nodes + t0 + t) * p.num_kv_heads + g) * D + 8 * ch);
+      }
+      if (__builtin_expect(odd, 0)) {
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if ((x[j][i] & 0x7F80u) == 0x7F80u) x[j][i] &= 0xFFFF0000u;
+            if ((x[j][i] & 0x7F800000u) == 0x7F800000u) x[j][i] &= 0xFFFFu;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int e = thread + THREADS * (k + j), t = e / (D / 8), ch = e - t * (D / 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[j][i] & 0x7FFF7FFFu));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          *(uint16_t*)(vt + tree_v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
+              (uint16_t)(x[j][i >> 1] >> (16 * (i & 1)));
+      }
+    }
+    if (__builtin_expect(!__any(top[0] >= 0x7F80 || top[1] >= 0x7F80), 1)) return odd;
+    odd = true;
+  }
+}
+
+// What the drafts that the lane's column attends (`sees`) add to its 4 values from head dim d0 on: the
+// sum of their values that are not finite, else 0.
+__device__ __forceinline__ f32x4 tree_odd_values(const TreeParams& p, int D, int b, int g, uint64_t sees,
+                                                 int d0) {
+  f32x4 sum{0.f, 0.f, 0.f, 0.f};
+  for (; sees; sees &= sees - 1) {
+    const int t = __builtin_ctzll(sees);
+    const u32x2 w = *(const u32x2*)(p.v_draft + (((int64_t)b * p.num_nodes + t) * p.num_kv_heads + g) * D + d0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t v = (w[e >> 1] >> (16 * (e & 1))) & 0xFFFFu;
+      if ((v & 0x7F80u) == 0x7F80u) sum[e] += __uint_as_float(v << 16);
+    }
+  }
+  return sum;
+}
+
+// Head dim of the first of a lane's 4 values in accumulator quad `quad`.
+__device__ __forceinline__ int tree_quad_dim(int quad, int h) { return 32 * (quad >> 2) + 8 * (quad & 3) + 4 * h; }
+
+// Adds tree_odd_values to a quad that this lane has stored: 4 outputs in bf16, or 4 values of a partial.
+template <typename Quad>
+__device__ __forceinline__ void tree_add_odd(Quad* at, f32x4 odd) {
+  Quad o = *at;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (odd[e] != 0.f) o[e] = (float)o[e] + odd[e];
+  *at = o;
 }
 
 }  // namespace dora

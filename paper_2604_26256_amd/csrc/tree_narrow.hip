@@ -24,6 +24,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
   typedef TreeTokens<P, FP8> Tok;
   __shared__ __align__(16) f32x4 s_o[kTreeWaves][QUADS][64];  // merge; a wave's draft V before
   __shared__ float2 s_ml[kTreeWaves][32];
+  __shared__ int s_odd[kTreeWaves];
   extern __shared__ int s_pre[];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
@@ -179,22 +180,13 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     }
 
     // Drafts (the last stages).  V is turned round through the wave's part of LDS.
+    bool odd = false;  // among V of the wave's drafts, something is not finite
     for (int st = a > cache_stages ? a : cache_stages; st < z; ++st) {
       // the wave with the fewest cache steps first
       const int t0 = ((st - cache_stages) * SP + SP - 1 - wave) * 32;
       if (t0 >= nodes) continue;  // uniform in the wave
       uint8_t* vt = (uint8_t*)&s_o[wave][0][0];  // [d][32 nodes]
-      for (int e = lane; e < 32 * (D / 8); e += 64) {
-        const int t = e / (D / 8), ch = e - t * (D / 8);
-        u32x4 vx{0u, 0u, 0u, 0u};
-        if (t0 + t < nodes)
-          vx = *(const u32x4*)(p.v_draft +
-                               (((int64_t)b * p.num_nodes + t0 + t) * Hkv + g) * D + 8 * ch);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          *(uint16_t*)(vt + tree_v_at(8 * ch + i, t >> 3) + 2 * (t & 7)) =
-              (uint16_t)(vx[i >> 1] >> (16 * (i & 1)));
-      }
+      odd |= tree_put_drafts<D, 64>(p, vt, b, g, t0, nodes, lane);
       const int t = t0 + ktok < nodes ? t0 + ktok : nodes - 1;  // a row past the nodes is masked
       const uint16_t* kd = p.k_draft + (((int64_t)b * p.num_nodes + t) * Hkv + g) * D;
       auto vf = [&](int i, int s) -> bf16x8 {
@@ -211,9 +203,14 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
     const int64_t slot = 2 * (int64_t)place + (first_piece ? 0 : 1);
     float S = sum_xor32(l_run), M = m_run;
     if (h == 0) s_ml[wave][col] = make_float2(m_run, S);
+    if (lane == 0) s_odd[wave] = odd;
     __syncthreads();  // and every wave has done with its drafts
+    int any_odd = 0;
 #pragma unroll
-    for (int w = 0; w < SP; ++w) M = fmaxf(M, s_ml[w][col].x);
+    for (int w = 0; w < SP; ++w) {
+      M = fmaxf(M, s_ml[w][col].x);
+      any_odd |= s_odd[w];
+    }
     S = 0.f;
 #pragma unroll
     for (int w = 0; w < SP; ++w) {
@@ -242,6 +239,16 @@ __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_
         *(bf16x4*)(p.out + row * D + 32 * i + 8 * j + 4 * h) =
             bf16x4{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv),
                    (__bf16)(o[3] * inv)};
+    }
+    if (__builtin_expect(uni(any_odd), 0)) {
+      for (int quad = wave; quad < QUADS; quad += SP) {
+        const int d0 = tree_quad_dim(quad, h);
+        const f32x4 add = tree_odd_values(p, D, b, g, sees, d0);
+        if (!whole)
+          tree_add_odd(&((f32x4*)(p.part_o + slot * 32 * D))[quad * 64 + lane], add);
+        else if (mine)
+          tree_add_odd((bf16x4*)(p.out + row * D + d0), add);
+      }
     }
     if (!whole && wave == 0 && h == 0) p.part_ml[slot * 32 + col] = make_float2(M, S);
     if (!whole && a == 0 && tid == 0)

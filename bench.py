@@ -83,7 +83,7 @@ KERNEL_SOURCES = [os.path.join(ROOT, "paper_2604_26256_amd", "csrc", f)
                             "tree.hip", "tree_narrow.hip", "tree_core.h", "window.hip",
                             "append_path.hip", "page_copy.hip",
                             "decode_core.h", "merge_core.h", "fp8_core.h", "dora_internal.h",
-                            "cache_internal.h", "api.cpp")]
+                            "cache_internal.h", "cache_rules.h", "api.cpp")]
 
 
 def _code_only(text: str) -> str:

@@ -6,12 +6,11 @@
 #include <stdint.h>
 
 #include "cache_internal.h"
+#include "cache_rules.h"
 
 using namespace dora;
 
 namespace {
-
-size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
@@ -51,101 +50,8 @@ int64_t page_bytes_of(const dora_decode_desc& d) {
          (d.kv_dtype == DORA_KV_FP8_E4M3 ? 1 : 2);
 }
 
-// ---------------------------------------------------------------------------
-// tree
-// ---------------------------------------------------------------------------
-
-struct TreeLayout {
-  int tiles, blocks;   // column tiles of a workgroup, column blocks of a (sequence, KV head)
-  int seqs;            // sequences of a launch
-  int64_t workgroups;  // of a launch
-  size_t cuts_off, part_o_off, part_ml_off, total;
-};
-
 dora_status check_nodes(int32_t num_nodes) {
   return num_nodes < 1 || num_nodes > 64 ? DORA_ERR_INVALID_ARG : DORA_OK;
-}
-
-void tree_layout(const dora_decode_desc& d, int32_t num_nodes, TreeLayout* t) {
-  const int64_t columns = (int64_t)num_nodes * (d.num_q_heads / d.num_kv_heads);
-  t->tiles = tree_tiles(columns);
-  t->blocks = (int)((columns + 32 * t->tiles - 1) / (32 * t->tiles));
-  // A launch's stages (a segment's start counts as some) are counted in 32 bits; one row's, of
-  // less than 2^19 pages, 128 heads and 9 blocks, always fit.
-  const int64_t steps = ((int64_t)d.block_table_stride * d.page_size + 31) / 32 + 2 + 8;
-  int64_t seqs = INT32_MAX / (steps * d.num_kv_heads * t->blocks);
-  if (seqs > kTreeMaxSeqs) seqs = kTreeMaxSeqs;
-  t->seqs = (int)(seqs < d.num_seqs ? seqs : d.num_seqs);
-  // Workgroups a CU.  One tile: two, but one where a wave holds two bf16 steps of 128 dims in
-  // registers (92 us against 123 with half the registers).  Two tiles, of two waves: three (the 64
-  // fp8 columns of 256 rows 500 us, 588 with two, 520 with four; bf16's LDS has no room for four).
-  const bool large = d.head_dim == 128 && d.kv_dtype == DORA_KV_BF16;
-  const int waves = t->tiles == 2 ? 2 : kTreeWaves;  // of a workgroup
-  const int per_cu = t->tiles < 2 ? (large ? 1 : 2) : t->tiles == 2 ? 3 : 2;
-  const int64_t slots = (int64_t)compute_units() * per_cu;
-  const int64_t most = (int64_t)t->seqs * d.num_kv_heads * t->blocks * steps;
-  t->workgroups = d.num_waves > 0 ? ((int64_t)d.num_waves + waves - 1) / waves
-                  : slots < most ? slots : most;
-  if (t->workgroups < 1) t->workgroups = 1;
-  size_t off = kWsHeaderBytes;
-  t->cuts_off = off;
-  off = align_up(off + (size_t)t->workgroups * 16);
-  t->part_o_off = off;
-  off = align_up(off + (size_t)(2 * t->workgroups) * t->tiles * 32 * d.head_dim * 4);
-  t->part_ml_off = off;
-  off = align_up(off + (size_t)(2 * t->workgroups) * t->tiles * 32 * 8);
-  t->total = off;
-}
-
-// Whether a launch takes a workgroup per (sequence, KV head, column block), uncut: where no row
-// is longer than 2,048 tokens and, with more than one tile (whose workgroups take all of a row's
-// steps one by one), the workgroups fill the chip or no row passes 512.  Against equal ranges and
-// their join: one tile, 128 fp8 rows of 400 tokens at the median, 8 heads of 128, 43 us for 53, 8 bf16 rows
-// of 1,024, 2 heads of 64, 10.2 for 12.5, of 4,096, 23 for 17; two tiles, 256 bf16 rows of up to
-// 1,024, 4 heads, 60 for 67, 64 of 2,048, 62 for 76, but 4 fp8 rows of 1,024, 8 heads, 30 for 25, of
-// 2,048, 52 for 31.
-bool tree_whole(const dora_decode_desc& d, const TreeLayout& t, int seqs) {
-  const int64_t tokens = (int64_t)d.block_table_stride * d.page_size;
-  const int64_t groups = (int64_t)seqs * d.num_kv_heads * t.blocks;
-  return d.num_waves <= 0 &&
-         (tokens <= 512 || (tokens <= 2048 && (t.tiles < 2 || groups >= compute_units())));
-}
-
-// ---------------------------------------------------------------------------
-// window
-// ---------------------------------------------------------------------------
-
-struct WindowLayout {
-  int chunk_pages, chunks;
-  size_t part_o_off, part_ml_off, total;
-};
-
-// Pages that a sequence can show, at most.
-int64_t most_visible(const dora_decode_desc& d, int32_t window, int32_t sinks) {
-  const int64_t P = d.page_size;
-  const int64_t n = (window + P - 2) / P + 1 + (sinks + P - 1) / P;
-  return n < d.block_table_stride ? n : d.block_table_stride;
-}
-
-void window_layout(const dora_decode_desc& d, int32_t window, int32_t sinks, WindowLayout* w) {
-  const int64_t most = most_visible(d, window, sinks);
-  const int seqs = d.num_seqs < kMaxSeqsPerLaunch ? d.num_seqs : kMaxSeqsPerLaunch;
-  const int64_t segs = (int64_t)seqs * d.num_kv_heads;
-  int64_t chunk = segs > 0 ? (most * segs + 1023) / 1024 : most;  // about 1,024 workgroups
-  const int64_t least = 256 / d.page_size;
-  chunk = (chunk + least - 1) / least * least;
-  if (chunk > 64 * kSegWaves) chunk = 64 * kSegWaves;  // a lane holds each page of its wave
-  if (chunk > most) chunk = most;
-  w->chunk_pages = (int)chunk;
-  w->chunks = (int)((most + chunk - 1) / chunk);
-  size_t off = kWsHeaderBytes;
-  const size_t slots = w->chunks > 1 ? (size_t)segs * w->chunks : 0;
-  const size_t G = (size_t)(d.num_q_heads / d.num_kv_heads);
-  w->part_o_off = off;
-  off = align_up(off + slots * G * d.head_dim * 4);
-  w->part_ml_off = off;
-  off = align_up(off + slots * G * 8);
-  w->total = off;
 }
 
 dora_status check_window(int32_t window, int32_t sinks) {
@@ -173,7 +79,7 @@ extern "C" {
 size_t dora_decode_tree_workspace_bytes(const dora_decode_desc* desc, int32_t num_nodes) {
   if (check_desc(desc) != DORA_OK || check_nodes(num_nodes) != DORA_OK) return 0;
   TreeLayout t;
-  tree_layout(*desc, num_nodes, &t);
+  tree_layout(*desc, num_nodes, compute_units(), &t);
   return t.total;
 }
 
@@ -194,8 +100,9 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
   if (st != DORA_OK) return st;
   if (!k_draft || !v_draft || !tree_mask || !aligned16(k_draft) || !aligned16(v_draft))
     return DORA_ERR_INVALID_ARG;
+  const int cus = compute_units();
   TreeLayout t;
-  tree_layout(d, num_nodes, &t);
+  tree_layout(d, num_nodes, cus, &t);
   if (workspace_bytes < t.total) return DORA_ERR_WORKSPACE_TOO_SMALL;
   hipStream_t s = (hipStream_t)stream;
   uint8_t* ws = (uint8_t*)workspace;
@@ -229,7 +136,7 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
     p.group = d.num_q_heads / d.num_kv_heads;
     p.stride = d.block_table_stride;
     p.blocks = t.blocks;
-    p.whole = tree_whole(d, t, p.num_seqs) ? 1 : 0;
+    p.whole = tree_whole(d, t, p.num_seqs, cus) ? 1 : 0;
     p.page_bytes = page_bytes_of(d);
     p.scale_log2 = scale_log2_of(d);
     const int64_t grid =

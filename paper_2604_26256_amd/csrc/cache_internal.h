@@ -15,6 +15,12 @@ namespace dora {
 constexpr int kTreeWaves = 4;        // waves of a workgroup (with two tiles: two)
 constexpr int kTreeMaxSeqs = 2048;   // sequences of a launch: their stage prefix lives in LDS
 
+// What a segment costs besides its steps (lengths, page ids, queries, the merge or the rows).  One
+// tile, in stages of four steps: the bf16 rows at its kernel 92 us against 105 at 0.  More, in
+// steps: 256 fp8 rows of 2,048 tokens at the median, 8 nodes, 492 us, 510 at 8, 530 at 4.
+constexpr int kTreeNarrowCost = 2;
+constexpr int kTreeWideCost = 12;
+
 // Tiles of 32 columns (a node's query heads, node by node) of a workgroup, for `columns` =
 // nodes x group.  28 columns in one tile 92 us, through LDS in two 114; 56 in two tiles 122, in four
 // 130 (bf16; fp8, 32 and 64 columns: 371 and 431, 539 and 621; the rows are at the kernels).

@@ -27,10 +27,11 @@ inline void tree_layout(const dora_decode_desc& d, int32_t num_nodes, int cus, T
   const int64_t columns = (int64_t)num_nodes * (d.num_q_heads / d.num_kv_heads);
   t->tiles = tree_tiles(columns);
   t->blocks = (int)((columns + 32 * t->tiles - 1) / (32 * t->tiles));
-  // A launch's stages (a segment's start counts as some) are counted in 32 bits; one row's, of
-  // less than 2^19 pages, 128 heads and 9 blocks, always fit.
-  const int64_t steps = ((int64_t)d.block_table_stride * d.page_size + 31) / 32 + 2 + 8;
-  int64_t seqs = INT32_MAX / (steps * d.num_kv_heads * t->blocks);
+  // A launch's stages (steps, at most, and a segment's start) are counted in 32 bits, with room for
+  // their rounding to ranges; one row's, of less than 2^19 pages, 128 heads and 9 blocks, always fit.
+  const int64_t steps = ((int64_t)d.block_table_stride * d.page_size + 31) / 32 + 2 +
+                        (kTreeWideCost > kTreeNarrowCost ? kTreeWideCost : kTreeNarrowCost);
+  int64_t seqs = (INT32_MAX - 64) / (steps * d.num_kv_heads * t->blocks);
   if (seqs > kTreeMaxSeqs) seqs = kTreeMaxSeqs;
   t->seqs = (int)(seqs < d.num_seqs ? seqs : d.num_seqs);
   // Workgroups a CU.  One tile: two, but one where a wave holds two bf16 steps of 128 dims in

@@ -13,9 +13,6 @@ namespace dora {
 
 // Pages whose ids (and fp8 scales) a workgroup holds in LDS at a time.
 constexpr int kTreeWindow = 512;
-// What a segment costs besides its steps (lengths, page ids, queries, the rows), in steps; 256
-// fp8 rows of 2,048 tokens at the median, 8 nodes: 492 us, 510 at 8, 530 at 4.
-constexpr int kTreeWideCost = 12;
 
 // Waits until at most N of the wave's loads are under way.
 template <int N>

@@ -10,10 +10,6 @@
 
 namespace dora {
 
-// What a segment costs besides its stages (lengths, page ids, queries, the merge), in stages: the
-// bf16 rows above 92 us against 105 at 0.
-constexpr int kTreeNarrowCost = 2;
-
 template <int D, int P, bool FP8>
 __global__ __launch_bounds__(64 * kTreeWaves, FP8 || D == 64 ? 2 : 1) void tree_narrow_kernel(TreeParams p) {
   constexpr int SP = kTreeWaves, PAIR = 32 / P;

@@ -92,7 +92,11 @@ inline void window_layout(const dora_decode_desc& d, int32_t window, int32_t sin
   int64_t chunk = segs > 0 ? (most * segs + 1023) / 1024 : most;  // about 1,024 workgroups
   const int64_t least = 256 / d.page_size;
   chunk = (chunk + least - 1) / least * least;
-  if (chunk > 64 * kSegWaves) chunk = 64 * kSegWaves;  // a lane holds each page of its wave
+  // A lane holds each page of its wave.  What a window has beyond 256 pages, be it one, is a part of
+  // its own: level with equal parts (128 rows of 8,000 tokens through 4,096, 8 heads of 128, pages of
+  // 16: bf16 345 us, 351 in equal parts, fp8 206 and 211) or faster (400 rows, fp8, 612 and 642), as the
+  // few short workgroups run beside the rest, and rows of 130 to 256 pages stay whole.
+  if (chunk > 64 * kSegWaves) chunk = 64 * kSegWaves;
   if (chunk > most) chunk = most;
   w->chunk_pages = (int)chunk;
   w->chunks = (int)((most + chunk - 1) / chunk);

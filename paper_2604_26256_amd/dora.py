@@ -576,14 +576,23 @@ def dora_kv_append(k_new, v_new, block_table, seq_lens, k_pages, v_pages, *, num
            "dora_kv_append")
 
 
+def _i32(name, value):
+    """value as the library takes it: a larger one would lose its upper bits on the way."""
+    value = int(value)
+    if not -2**31 <= value < 2**31:
+        raise ValueError(f"{name} must fit 32 bits, got {value}")
+    return value
+
+
 def dora_decode_tree_workspace_bytes(desc: dora_decode_desc, num_nodes) -> int:
     """Workspace of dora_decode_attn_tree (0 on invalid arguments)."""
-    return int(_lib.dora_decode_tree_workspace_bytes(ctypes.byref(desc), int(num_nodes)))
+    return int(_lib.dora_decode_tree_workspace_bytes(ctypes.byref(desc), _i32("num_nodes", num_nodes)))
 
 
 def dora_decode_window_workspace_bytes(desc: dora_decode_desc, window, sinks) -> int:
     """Workspace of dora_decode_attn_window (0 on invalid arguments)."""
-    return int(_lib.dora_decode_window_workspace_bytes(ctypes.byref(desc), int(window), int(sinks)))
+    return int(_lib.dora_decode_window_workspace_bytes(ctypes.byref(desc), _i32("window", window),
+                                                       _i32("sinks", sinks)))
 
 
 def _marshal(device, stream, specs):
@@ -750,9 +759,7 @@ def dora_decode_attn_window(q, k_pages, v_pages, block_table, seq_lens, version_
     num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B][stride]")
-    window, sinks = int(window), int(sinks)
-    if not -2**31 <= window < 2**31 or not -2**31 <= sinks < 2**31:
-        raise ValueError("window and sinks are 32-bit token counts")
+    window, sinks = _i32("window", window), _i32("sinks", sinks)
     if kv_dtype != DORA_KV_FP8_E4M3:
         k_scales = v_scales = None
     elif B:
@@ -1045,6 +1052,7 @@ class Pool:
         if num_tokens is None:
             num_tokens = self.seq_info(seq_id)[0]
         new_id, src, dst, n = ctypes.c_int64(), ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
+        num_tokens = _i32("num_tokens", num_tokens)
         _check(_lib.dora_pool_fork_seq(self._h, seq_id, num_tokens, ctypes.byref(new_id),
                                        ctypes.byref(src), ctypes.byref(dst), ctypes.byref(n)),
                "dora_pool_fork_seq")
@@ -1053,7 +1061,7 @@ class Pool:
 
     def release_window(self, seq_id: int, window: int, sinks: int = 0) -> int:
         """Release the pages of seq_id that no later window decode reads; how many it released."""
-        n = ctypes.c_int32()
+        n, window, sinks = ctypes.c_int32(), _i32("window", window), _i32("sinks", sinks)
         _check(_lib.dora_pool_release_window(self._h, seq_id, window, sinks, ctypes.byref(n)),
                "dora_pool_release_window")
         return n.value

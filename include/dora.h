@@ -544,13 +544,17 @@ dora_status dora_pool_fork_seq(dora_pool* pool, int64_t seq_id, int32_t num_toke
 /* Release the pages of a sequence that no later dora_decode_attn_window call with this
  * window and these sinks reads (window >= 1, sinks >= 0): those that lie whole between
  * the sinks and the window of the newest token.  Its tokens still count, its table keeps
- * its width; it is for dora_decode_attn_window from then on.  *n_out (may be NULL): pages released by this sequence in this call. */
+ * its width; it is for dora_decode_attn_window from then on.  Call it once the tokens that
+ * the sequence counts are stored: dora_kv_append_path of more of them than the window holds
+ * would find 0 for a released page, and write what may be another sequence's.
+ * *n_out (may be NULL): pages released by this sequence in this call. */
 dora_status dora_pool_release_window(dora_pool* pool, int64_t seq_id, int32_t window,
                                      int32_t sinks, int32_t* n_out);
 /* Move live pages from the pool's end into its free places, so that the n live pages
  * are pages 0 .. n - 1: fills src_pages and dst_pages (cap entries; *n_out of them) for
  * one dora_kv_page_copy per layer and renames the pages in every sequence; block tables
- * taken before are stale.  Afterwards pages are handed out in increasing order.
+ * taken before are stale, and so are page ids of forks and migrations whose copies are not
+ * yet made.  Afterwards pages are handed out in increasing order.
  * DORA_ERR_WORKSPACE_TOO_SMALL (more than cap moves; *n_out says how many) leaves the
  * pool unchanged. */
 dora_status dora_pool_compact(dora_pool* pool, int32_t* src_pages, int32_t* dst_pages, int32_t cap,

@@ -1060,7 +1060,8 @@ class Pool:
                 np.array([dst.value], np.int32)[:n.value])
 
     def release_window(self, seq_id: int, window: int, sinks: int = 0) -> int:
-        """Release the pages of seq_id that no later window decode reads; how many it released."""
+        """Release the pages of seq_id that no later window decode reads, once its tokens are stored;
+        how many it released."""
         n, window, sinks = ctypes.c_int32(), _i32("window", window), _i32("sinks", sinks)
         _check(_lib.dora_pool_release_window(self._h, seq_id, window, sinks, ctypes.byref(n)),
                "dora_pool_release_window")
@@ -1068,7 +1069,7 @@ class Pool:
 
     def compact(self):
         """Move the live pages to the pool's start.  Returns (src_pages, dst_pages) to copy with
-        dora_kv_page_copy; block tables taken before are stale."""
+        dora_kv_page_copy; block tables taken before are stale, as are page ids of copies not yet made."""
         src, dst = np.zeros(self.num_pages, np.int32), np.zeros(self.num_pages, np.int32)
         n = ctypes.c_int32()
         _check(_lib.dora_pool_compact(self._h, src.ctypes.data_as(_P), dst.ctypes.data_as(_P),

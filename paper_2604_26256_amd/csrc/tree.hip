@@ -379,9 +379,9 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeParams p) {
 }
 
 // CODES where vector instructions bound the waves (four tiles) and rows may be long enough for the
-// queries' codes, about 1 us a segment.  256 fp8 rows of 6,000 tokens, 128 columns: 943 us against
-// 1,003; of 1,500 tokens (800 rows) 843 against 850, of 700 level; in two tiles or whole rows of 500
-// slower by 4 to 5%.
+// queries' codes, about 1 us a segment.  128 columns, fp8, against the widened codes: rows of 6,000 tokens
+// (256) 962 us for 1,024 (128 dims, pages of 32), 1,014 for 1,061 (16), 64 dims 626 for 658 and 690 for
+// 706; rows of 1,500 (800) and 700 (1,600) level; in two tiles or whole rows of 500 slower by 4 to 5%.
 template <int D, int P, bool FP8>
 static const void* wide_fn(int tiles, bool whole) {
   if constexpr (FP8)

@@ -37,7 +37,7 @@ __device__ __forceinline__ void tree_fetch(const uint8_t* from, uint8_t* to) {
 // bf16 rows).  A fourth buffer: 1,000 and 140 us, but 137 for 124 in the 56-column rows.
 //   Bound by no one unit: two waves a SIMD, whose vector and matrix instructions overlap in part.
 // 256 fp8 rows of 4,096 tokens at the median, 16 nodes, 64/8 heads of 128 dims (128 columns): 3.3 GB
-// and 0.80 TFLOP in 973 us with CODES, 0.82 PFLOP/s (a large bf16 product 1.34).  5 bf16 rows of 30,000, up to
+// and 0.80 TFLOP in 973 us with CODES, 0.82 PFLOP/s without the join of 25 us (a large bf16 product 1.34).  5 bf16 rows of 30,000, up to
 // 64 nodes, 32/8 heads: 139 us, 0.5 PFLOP/s.  64 bf16 rows of 2,048 at the median, up to 8 nodes,
 // 28/4 heads (56 columns): 0.50 GB in 124 us.  What does not pay: two tiles a wave straight from HBM
 // (rows of 6,000 981 us instead of 1,010, of 500 1,440 instead of 960), registers for three waves

@@ -10,7 +10,7 @@ from gpu_util import lib
 pytestmark = pytest.mark.gpu
 
 
-def _run(c, T, G, counts, seed, odd=False, roundings=1, **kw):
+def _run(c, T, G, counts, seed, roundings=1, **kw):
     print(f"[case] n={len(c.lens)} T={T} G={G} d={c.d} P={c.P} dt={c.dt} stride={c.bt.shape[1]} {kw}", flush=True)
     assert c.bt.shape[1] * c.P > 2048, "whole rows"
     B, g = len(c.lens), torch.Generator().manual_seed(seed)

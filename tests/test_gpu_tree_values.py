@@ -77,3 +77,19 @@ def test_one_branch_does_not_change_the_others(T, G):
         got, _ = _check(c, q, kd, vd, mask, [T] * 3)
         assert torch.equal(got[:, :half].view(torch.int16), clean[:, :half].view(torch.int16))
         assert not torch.isfinite(got[:, half:].float()).any()
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("G", [1, 2, 4])
+@pytest.mark.parametrize("waves", [1, 6, 40, 4000])
+def test_ranges_that_end_between_drafts(waves, G, dt):
+    """The two steps of 64 drafts in one workgroup's piece and in two's: a piece adds what is odd in its
+    own, where another's may weigh nothing."""
+    c = Cache([40, 7, 0, 700, 33], 2, 64, 16, dt, seed=9)
+    mask = random_trees(np.random.default_rng(4), [64] * 5, 64)
+    mask[2, 5] = 1 << 40  # a node that attends one of the second step alone
+    mask[2, 6] = 1 << 3
+    q, kd, vd = _inputs(5, 64, 2, G, 64, 6)
+    for j, value in ((3, INF), (20, NAN), (40, -INF), (63, INF)):
+        vd[:, j, :, j % 7:j % 7 + 2] = value
+    _check(c, q, kd, vd, mask, [64] * 5, num_waves=waves)

@@ -317,7 +317,7 @@ def run(s):
 
 def _kw(s):
     case, pool = s["case"], s["pool"]
-    return {"num_kv_heads": case["kv_heads"], "page_size": case["page"], "kv_dtype": ("bf16", "fp8", "fp4").index(case["dtype"]), "k_scales": pool["k_scales"]}
+    return {"num_kv_heads": case["kv_heads"], "page_size": case["page"], "kv_dtype": {"bf16": 0, "fp8": 1, "fp4": 4}[case["dtype"]], "k_scales": pool["k_scales"]}
 
 
 def _bounds_of(bounds, case):

@@ -81,9 +81,12 @@ COMPUTE_CMD = ("cd /tmp && timeout -s KILL 300 rocprofv3 --pmc {c} --output-form
 KERNEL_SOURCES = [os.path.join(ROOT, "paper_2604_26256_amd", "csrc", f)
                   for f in ("decode.hip", "segment.hip", "grouped.hip", "append.hip", "pack.hip",
                             "tree.hip", "tree_narrow.hip", "tree_core.h", "window.hip",
-                            "append_path.hip", "page_copy.hip",
-                            "decode_core.h", "merge_core.h", "fp8_core.h", "dora_internal.h",
-                            "cache_internal.h", "cache_rules.h", "api.cpp")]
+                            "append_path.hip", "page_copy.hip", "append4.hip", "decode4.hip",
+                            "pages.hip", "select.hip",
+                            "decode_core.h", "merge_core.h", "fp8_core.h", "fp4_core.h",
+                            "bits_core.h", "path_core.h", "ranges_core.h", "api_checks.h",
+                            "dora_internal.h", "cache_internal.h", "pages_internal.h",
+                            "cache_rules.h", "api.cpp")]
 
 
 def _code_only(text: str) -> str:

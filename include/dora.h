@@ -44,10 +44,20 @@
  *   k_scales, v_scales  [num_pages] fp32 (fp8 only): stored value times the
  *                page's scale is the key/value (one scale per page, shared by
  *                all heads and tokens of that page)
+ *   4-bit pages (DORA_KV_FP4): k_pages, v_pages [num_pages][num_kv_heads] tiles of
+ *                page_size * head_dim * 17 / 32 bytes, scales among them:
+ *                K  E2M1 codes [head_dim / 32][page_size][32], two in a byte (the
+ *                   even one in its low half), then for each 32 dims of a token
+ *                   the exponent, biased by 127, of the power of two that the
+ *                   codes are times: bytes [head_dim / 32][page_size / 16][4][4],
+ *                   that of slot 16 a + 4 b + c at [a][c][b]; 255 stands for NaN
+ *                V  E2M1 codes [head_dim][page_size], two in a byte, then a bf16
+ *                   scale for each 64 dims of a token [head_dim / 64][page_size]
  *   block_table  [num_seqs][block_table_stride] int32 page ids, logical order
  *   seq_lens     [num_seqs] int32, tokens to attend (>= 0)
  *   version_ids  [num_seqs] int32 policy version of each sequence
- * fp8 is OCP E4M3FN (bias 7, max 448, S.1111.111 = NaN, no infinity).
+ * fp8 is OCP E4M3FN (bias 7, max 448, S.1111.111 = NaN, no infinity).  E2M1 codes
+ * stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6 and, with bit 3 set, their negatives.
  * GQA mapping: query head h reads KV head h / (num_q_heads / num_kv_heads).
  * Slots of the last page beyond seq_lens[b] are never used in the arithmetic
  * (they may hold any bytes, NaN included).
@@ -87,7 +97,9 @@ typedef enum {
 
 typedef enum {
   DORA_KV_BF16 = 0,
-  DORA_KV_FP8_E4M3 = 1
+  DORA_KV_FP8_E4M3 = 1,
+  DORA_KV_FP4 = 4            /* E2M1 codes with scales in the pages; tree, window and
+                                grouped attention are not built for it */
 } dora_kv_dtype;
 
 /* Flags for dora_decode_desc.flags. */
@@ -97,7 +109,8 @@ typedef enum {
 
 /* Geometry and options of one decode-attention call.  Supported builds:
  * head_dim in {64, 128}; page_size in {16, 32}; group size num_q_heads /
- * num_kv_heads in [1, 16]; kv_dtype bf16 or fp8 e4m3. */
+ * num_kv_heads in [1, 16]; kv_dtype bf16, fp8 e4m3 or 4-bit (where a call does not
+ * say otherwise). */
 typedef struct {
   int32_t num_seqs;            /* B >= 0 */
   int32_t num_q_heads;         /* Hq, multiple of num_kv_heads */
@@ -115,16 +128,18 @@ typedef struct {
   uint32_t flags;              /* DORA_FLAG_* */
   int32_t num_waves;           /* decode wavefronts to launch; 0 = library
                                   default: per compute unit of the current
-                                  device at most 4 for bf16 pages and 7 for
-                                  fp8 pages, within the resident wavefront
-                                  slots; never more than the batch can use
+                                  device at most 4 for bf16 pages, 7 for
+                                  fp8 pages and 8 for 4-bit ones, within the
+                                  resident wavefront slots; never more than the
+                                  batch can use
                                   (B x Hkv x stride page-heads over the minimum
                                   range).  With both this and min_range_pages 0,
                                   batches whose block tables are short or few
                                   are cut per segment instead (see
                                   dora_decode_attn) */
   int32_t min_range_pages;     /* smallest work range per wavefront, in
-                                  (page, KV head) units; 0 = library default */
+                                  (page, KV head) units, of 4-bit pages in (64
+                                  tokens, KV head); 0 = library default */
 } dora_decode_desc;
 
 /* Human-readable name of a status code (static storage); "unknown status" for
@@ -149,7 +164,7 @@ size_t dora_decode_workspace_bytes(const dora_decode_desc* desc);
  * desc->min_range_pages or 8 when that is 0, and the first T mod W' ranges hold
  * one extra item; so a caller can tell which (sequence, KV head) segments a
  * call cuts across wavefronts (except batches cut per segment, see
- * dora_decode_attn).  Each launch covers at most 8192 sequences.
+ * dora_decode_attn).  Of 4-bit pages the work items are steps of 64 tokens.  Each launch covers at most 8192 sequences.
  * Returns 0 for an invalid or unsupported descriptor. */
 int64_t dora_decode_num_waves(const dora_decode_desc* desc);
 
@@ -324,6 +339,15 @@ dora_status dora_decode_attn_window(const dora_decode_desc* desc, int32_t window
  *   otherwise:                        s = s0       (s0: the page's scale)
  *   codes of the token: enc(x / s); the page's scale becomes s.
  * enc is the nearest OCP E4M3FN code, ties to even, saturating at +-448.
+ * 4-bit pages: no token depends on another.  With top the largest magnitude,
+ *   K, for each 32 dims: e = clamp(((bits of bf16 top + 0x20) >> 7) - 2, 1, 252) is the
+ *      exponent stored (top's own, less 2, and one more where its mantissa is 1.75 or
+ *      above), the codes are enc4(x / 2^(e - 127))
+ *   V, for each 64 dims: s = max(bf16(fp32(top / 6)), 2^-126), the codes are
+ *      enc4(fp32(x / s)); an infinite top counts as bf16's largest number
+ * enc4 is the nearest E2M1 value, ties to the even code, +-6 beyond (infinities too).
+ * A NaN makes its block NaN (exponent 255 or a NaN scale, codes 0).  The other half
+ * of a byte that holds two tokens' codes stays as it is.
  * The pages of one call must belong to distinct sequences (a page is never
  * appended to by two sequences at once).  Enqueued on `stream`; one launch
  * (two with dev_status). */
@@ -361,6 +385,101 @@ dora_status dora_kv_append_path(const dora_decode_desc* desc, int32_t num_tokens
                                 void* v_pages, float* k_scales, float* v_scales,
                                 int32_t* dev_status, dora_stream_t stream);
 
+/* Read the last tokens of every sequence back as bf16 rows: for n = counts[b]
+ * (num_tokens without counts) and L = seq_lens[b], row i < n of k_out[b] and v_out[b] is
+ * token L - n + i; rows behind it are left as they were.  bf16 pages give the values as
+ * they are; fp8 (code * scale) and 4-bit V (code * scale) are fp32 products rounded to
+ * bf16, 4-bit K is exact.
+ *   num_tokens   T in [1, DORA_PATH_MAX_TOKENS], rows of k_out and v_out per sequence
+ *   k_out, v_out device bf16 [B][T][Hkv][d], 16-byte aligned
+ *   counts       device int32 [B] in [0, T], or NULL
+ *   dev_status   as for dora_kv_append_path: what is skipped writes nothing
+ * The fp8 scales are desc's. */
+dora_status dora_kv_read(const dora_decode_desc* desc, int32_t num_tokens, const int32_t* counts,
+                         const void* k_pages, const void* v_pages, const int32_t* block_table,
+                         const int32_t* seq_lens, const int32_t* version_ids, void* k_out,
+                         void* v_out, int32_t* dev_status, dora_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention over the pages that a query wants most.  For a long sequence a step
+ * reads the bounds of its pages instead of the pages, chooses the pages that
+ * the bounds promise the largest scores, for each KV head, and attends those:
+ *   dora_kv_append[_path], then dora_kv_page_bounds over the same tokens;
+ *   dora_page_select; dora_decode_attn_pages.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of one page's bounds: for each KV head int8 [2][d], the largest and the smallest value
+ * of each dim in units of a scale, then, behind those of all heads, an fp32 scale for each;
+ * rounded up to 16.  0 for an unsupported geometry. */
+size_t dora_page_bounds_bytes(int32_t num_kv_heads, int32_t head_dim);
+
+/* Bounds of the keys of every page that the last n = counts[b] (num_tokens without counts)
+ * tokens of a sequence lie in, over the page's tokens t < L = seq_lens[b] (those before the
+ * last n too).  For each KV head, in fp32 with IEEE rounding, over the page's keys x:
+ *   s = max(max |x| / 127, 2^-126), largest[d] = ceil(max x_d / s), smallest[d] =
+ *   floor(min x_d / s), within +-127
+ * where a NaN (of 4-bit pages, a NaN block) counts as 0 and an infinity as bf16's largest
+ * number.  A page's bounds follow from its keys alone.
+ *   num_tokens   in [1, DORA_PATH_MAX_TOKENS]
+ *   bounds       device [num_pages] records of dora_page_bounds_bytes, 16-byte aligned
+ *   dev_status   as for dora_kv_append_path; a page that is skipped keeps its bounds
+ * The fp8 scales are desc's (v_scales is not used). */
+dora_status dora_kv_page_bounds(const dora_decode_desc* desc, int32_t num_tokens,
+                                const int32_t* counts, const void* k_pages,
+                                const int32_t* block_table, const int32_t* seq_lens,
+                                const int32_t* version_ids, void* bounds, int32_t* dev_status,
+                                dora_stream_t stream);
+
+/* Choose the pages that each (sequence, KV head) reads.  With N the pages of a sequence:
+ * all of them where N <= budget; else the first sink_pages, the last recent_pages, and of
+ * those between the budget - sink_pages - recent_pages with the largest scores (of equal
+ * ones the lower page).  The score of page j for KV head g is
+ *   s * max over the group's rows h of fp32(r_h * sum_d max(u_hd lo_d, u_hd hi_d))
+ * with hi, lo, s the page's bounds and the row as whole numbers u_hd = rint(q_hd / r_h), r_h
+ * = max(max |q_h| / 127, 2^-126): each operation in fp32 with IEEE rounding, the sum exact.
+ * So the choice depends on nothing but its inputs.  A NaN of q counts as 0.
+ *   desc         num_seqs, heads, head_dim, page_size, block_table_stride, num_pages;
+ *                kv_dtype and scales are not used; DORA_FLAG_VALIDATE checks the tables
+ *   budget       pages of a list, >= max(1, sink_pages + recent_pages), < 2^19
+ *   q            device bf16 [B][Hq][d]
+ *   bounds       device, as dora_kv_page_bounds writes them
+ *   page_lists   device int32 [B][Hkv][budget]: numbers of the sequence's pages (places in its
+ *                table's row), ascending; entries behind the count are left as they were
+ *   page_counts  device int32 [B][Hkv]: min(N, budget)
+ *   scores       device fp32 [B][Hkv][block_table_stride] or NULL: receives the scores of the
+ *                sequence's pages (entries behind them are left as they were)
+ *   workspace    >= dora_page_select_workspace_bytes(desc) bytes (with scores, 256), 16-byte aligned
+ * Two launches. */
+size_t dora_page_select_workspace_bytes(const dora_decode_desc* desc);
+dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32_t sink_pages,
+                             int32_t recent_pages, const void* q, const void* bounds,
+                             const int32_t* block_table, const int32_t* seq_lens,
+                             const int32_t* version_ids, int32_t* page_lists,
+                             int32_t* page_counts, float* scores, void* workspace,
+                             size_t workspace_bytes, dora_stream_t stream);
+
+/* Decode attention over listed pages: the operation of dora_decode_attn over the tokens t <
+ * seq_lens[b] of the pages page_lists[b][g][i], i < page_counts[b][g], alone, g the KV head.
+ * A list may be in any order; a page listed twice counts twice; an entry that is no page of
+ * the sequence (negative, or at or behind its last token) counts for nothing.  A row that
+ * attends nothing gives 0.  Only the table entries of listed pages are read.
+ *   list_stride  entries of a list, in [1, 2^19)
+ *   page_lists   device int32 [B][Hkv][list_stride], numbers of the sequence's pages
+ *   page_counts  device int32 [B][Hkv] in [0, list_stride] (values outside are taken as the
+ *                nearest inside)
+ *   desc         as for dora_decode_attn, any kv_dtype; num_waves and min_range_pages are not
+ *                used; DORA_FLAG_VALIDATE checks counts, entries and the listed pages' ids
+ *   workspace    >= dora_decode_pages_workspace_bytes(desc, list_stride) bytes
+ * Other arguments, flags and errors as for dora_decode_attn.  Repeated calls on the same inputs
+ * are bitwise identical. */
+size_t dora_decode_pages_workspace_bytes(const dora_decode_desc* desc, int32_t list_stride);
+dora_status dora_decode_attn_pages(const dora_decode_desc* desc, int32_t list_stride,
+                                   const void* q, const int32_t* page_lists,
+                                   const int32_t* page_counts, const void* k_pages,
+                                   const void* v_pages, const int32_t* block_table,
+                                   const int32_t* seq_lens, const int32_t* version_ids, void* out,
+                                   void* workspace, size_t workspace_bytes, dora_stream_t stream);
+
 /* ---------------------------------------------------------------------------
  * KV page pack / unpack: the device half of the paper's two-phase state
  * transfer for same-version migration (Sec. 3.4: request metadata travels by
@@ -377,7 +496,8 @@ dora_status dora_kv_append_path(const dora_decode_desc* desc, int32_t num_tokens
  *      24  int32    num_kv_heads
  *      28  int32    head_dim
  *      32  int64    n_pages
- *      40  int64    page_bytes   (= num_kv_heads * page_size * head_dim * e)
+ *      40  int64    page_bytes   (= num_kv_heads * page_size * head_dim * e; of
+ *                                 4-bit pages e = 17 / 32)
  *      48  int32    n_seqs       (caller's count of sequences in the list)
  *      52  int32    reserved (0); bytes 56..255 are 0
  *   then n_pages K pages (page_bytes each) in list order,

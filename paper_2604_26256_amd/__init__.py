@@ -6,9 +6,11 @@ The binding is loaded on first use, so ``paper_2604_26256_amd.build`` can run
 before the library exists.
 """
 _EXPORTS = (
-    "DORA_FLAG_VALIDATE", "DORA_KV_BF16", "DORA_KV_FP8_E4M3", "DoraError", "Pool",
+    "DORA_FLAG_VALIDATE", "DORA_KV_BF16", "DORA_KV_FP4", "DORA_KV_FP8_E4M3", "DoraError", "Pool",
     "PreparedDecode",
-    "dora_decode_attn", "dora_decode_attn_grouped", "dora_decode_workspace_bytes",
+    "dora_decode_attn", "dora_decode_attn_grouped", "dora_decode_attn_pages",
+    "dora_decode_workspace_bytes", "dora_kv_page_bounds", "dora_kv_read", "dora_page_bounds_bytes",
+    "dora_page_select",
     "dora_kv_append", "dora_kv_packed_bytes", "dora_kv_page_pack", "dora_kv_page_unpack",
     "make_decode_desc", "make_pack_desc", "plan_partition", "plan_supplement",
     "status_string",

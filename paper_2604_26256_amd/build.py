@@ -23,8 +23,9 @@ LIB = os.path.join(PKG, "libdora.so")
 ARCH = "gfx950"
 
 HIP_SOURCES = ["tree.hip", "tree_narrow.hip", "window.hip", "decode.hip", "segment.hip", "pack.hip",
-               "append.hip", "append_path.hip", "page_copy.hip", "grouped.hip", "measure.hip", "noalloc.hip"]
-CXX_SOURCES = ["api.cpp", "cache_api.cpp", "pool.cpp", "plan.cpp"]
+               "append.hip", "append_path.hip", "append4.hip", "page_copy.hip", "grouped.hip", "decode4.hip",
+               "pages.hip", "select.hip", "measure.hip", "noalloc.hip"]
+CXX_SOURCES = ["api.cpp", "cache_api.cpp", "pages_api.cpp", "pool.cpp", "plan.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", f"-I{INCLUDE}", f"-I{CSRC}"]
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -5,8 +5,11 @@
 #include <stdint.h>
 #include <string.h>
 
+#include "api_checks.h"
+#include "cache_internal.h"
 #include "dora_internal.h"
 #include "dora_measure.h"
+#include "pages_internal.h"
 
 using namespace dora;
 
@@ -16,12 +19,10 @@ constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
 bool geometry_supported(const dora_decode_desc& d) {
   if (d.head_dim != 64 && d.head_dim != 128) return false;
   if (d.page_size != 16 && d.page_size != 32) return false;
-  if (d.kv_dtype != DORA_KV_BF16 && d.kv_dtype != DORA_KV_FP8_E4M3) return false;
+  if (!kv_dtype_known(d.kv_dtype)) return false;
   const int G = d.num_q_heads / d.num_kv_heads;
   // the decode kernel's page-head descriptor holds g in 7 bits and j in 19, and
   // its page prefix and page-head indices are 32-bit
@@ -74,6 +75,21 @@ bool whole_segments(const dora_decode_desc& d, int64_t segs, int64_t tokens) {
   return segs - segs / d.num_kv_heads * 11 / 20 <= most;
 }
 
+// The same choice for 4-bit pages: pages of a workgroup of the listed-pages kernel, which then
+// takes all pages of a row, or 0 for the stream-K decode.
+int pages4_split(const dora_decode_desc& d, int64_t segs, int64_t waves) {
+  if (d.num_waves > 0 || d.min_range_pages > 0) return 0;
+  const int64_t tokens = (int64_t)d.block_table_stride * d.page_size;
+  auto fits = [&](int chunk, int64_t most) {  // each workgroup of a split has a partial slot
+    const int64_t workgroups = segs * ((tokens + chunk - 1) / chunk);
+    return workgroups <= most && workgroups <= 2 * waves;
+  };
+  if (tokens <= 1024 && segs <= 4096) return d.block_table_stride;
+  if (fits(256, 1024)) return 256 / d.page_size;
+  if (fits(512, 1024)) return 512 / d.page_size;
+  return 0;
+}
+
 // The split of the segment kernel for a launch over `segs` (sequence, KV head)
 // segments: pages per workgroup, or 0 where the stream-K decode runs instead.  A
 // caller that sets how the work is cut gets that cut.
@@ -102,6 +118,7 @@ bool whole_segments(const dora_decode_desc& d, int64_t segs, int64_t tokens) {
 // beyond, past 2,048 tokens, 0.93 (1.23, not taken); chunks of 512, fp8 up to 1,280
 // 0.57-0.83 (1.02), 2,048 for head dim 64 0.70 (0.99), bf16 up to 640 0.77 (1.10).
 int segment_split(const dora_decode_desc& d, int64_t segs, int64_t waves) {
+  if (d.kv_dtype == DORA_KV_FP4) return pages4_split(d, segs, waves);
   if (d.num_waves > 0 || d.min_range_pages > 0) return 0;
   const int64_t tokens = (int64_t)d.block_table_stride * d.page_size;
   const bool fp8 = d.kv_dtype == DORA_KV_FP8_E4M3;
@@ -158,20 +175,24 @@ namespace dora {
 int64_t decode_waves(const dora_decode_desc& d) {
   if (d.num_waves > 0) return d.num_waves;
   int dev = 0, cus = 0, per_cu = 0;
-  const bool fp8 = d.kv_dtype == DORA_KV_FP8_E4M3;
+  const bool fp8 = d.kv_dtype == DORA_KV_FP8_E4M3, fp4 = d.kv_dtype == DORA_KV_FP4;
   const int seqs = d.num_seqs < kMaxSeqsPerLaunch ? d.num_seqs : kMaxSeqsPerLaunch;
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
-      decode_waves_per_cu(d.head_dim, d.page_size, fp8, seqs, &per_cu) != hipSuccess ||
+      (fp4 ? decode4_waves_per_cu(d.head_dim, d.page_size, seqs, &per_cu)
+           : decode_waves_per_cu(d.head_dim, d.page_size, fp8, seqs, &per_cu)) != hipSuccess ||
       cus <= 0 || per_cu <= 0) {
     (void)hipGetLastError();  // no device here: size for a 256-CU part at 8 waves per CU
     cus = 256;
     per_cu = 8;
   }
-  const int cap = fp8 ? kFp8WavesPerCu : kBf16WavesPerCu;
+  const int cap = fp4 ? kFp4WavesPerCu : fp8 ? kFp8WavesPerCu : kBf16WavesPerCu;
   if (per_cu > cap) per_cu = cap;
   const int64_t slots = (int64_t)cus * per_cu;
-  const int64_t most = (int64_t)seqs * d.num_kv_heads * d.block_table_stride;
+  // page-heads, or of 4-bit pages steps of 64 tokens
+  const int64_t units =
+      fp4 ? ((int64_t)d.block_table_stride * d.page_size + 63) / 64 : d.block_table_stride;
+  const int64_t most = (int64_t)seqs * d.num_kv_heads * units;
   const int64_t need = (most + min_range_of(d) - 1) / min_range_of(d);
   return need < slots ? (need > 0 ? need : 1) : slots;
 }
@@ -298,6 +319,7 @@ bool grouped_layout(const dora_decode_desc& d, int32_t group_size, GroupedLayout
 
 // Host-checkable validity of the group arguments.
 dora_status check_groups(const dora_decode_desc& d, int32_t group_size) {
+  if (d.kv_dtype == DORA_KV_FP4) return DORA_ERR_UNSUPPORTED;
   if (group_size < 1 || d.num_seqs % group_size != 0) return DORA_ERR_INVALID_ARG;
   if ((int64_t)group_size * (d.num_q_heads / d.num_kv_heads) > kPrefixMaxColumns)
     return DORA_ERR_UNSUPPORTED;
@@ -314,9 +336,8 @@ dora_status enqueue_decode(const dora_decode_desc& d, const void* q, const void*
                            const int32_t* seq_lens, uint16_t* out, const GroupedSuffix* gs,
                            uint8_t* ws, const WsLayout& w, hipStream_t s, hipEvent_t* ev) {
   const GroupedParams* gp = gs ? gs->gp : nullptr;
-  const bool fp8 = d.kv_dtype == DORA_KV_FP8_E4M3;
+  const bool fp8 = d.kv_dtype == DORA_KV_FP8_E4M3, fp4 = d.kv_dtype == DORA_KV_FP4;
   const int G = d.num_q_heads / d.num_kv_heads;
-  const int e = fp8 ? 1 : 2;
   const float scale = d.sm_scale > 0.f ? d.sm_scale : 1.0f / sqrtf((float)d.head_dim);
   const int64_t qrow = (int64_t)d.num_q_heads * d.head_dim;  // elements per sequence
   if (ev && hipEventRecord(ev[0], s) != hipSuccess) return DORA_ERR_HIP;
@@ -349,9 +370,36 @@ dora_status enqueue_decode(const dora_decode_desc& d, const void* q, const void*
     dp.group = G;
     dp.stride = d.block_table_stride;
     dp.min_range = min_range_of(d);
-    dp.page_bytes = (int64_t)d.num_kv_heads * d.page_size * d.head_dim * e;
+    dp.page_bytes = page_bytes_of(d);
     dp.scale_log2 = scale * 1.4426950408889634f;
     const int seg_pages = gp ? 0 : segment_split(d, segs, w.waves);
+    if (seg_pages > 0 && fp4) {
+      PagesParams pp{};  // without lists: all pages of a row
+      pp.q = dp.q;
+      pp.k_pages = dp.k_pages;
+      pp.v_pages = dp.v_pages;
+      pp.block_table = dp.block_table;
+      pp.seq_lens = dp.seq_lens;
+      pp.out = dp.out;
+      pp.part_o = dp.part_o;
+      pp.part_ml = dp.part_ml;
+      pp.page_bytes = dp.page_bytes;
+      pp.num_seqs = nb;
+      pp.num_q_heads = d.num_q_heads;
+      pp.num_kv_heads = d.num_kv_heads;
+      pp.group = G;
+      pp.stride = d.block_table_stride;
+      pp.head_dim = d.head_dim;
+      pp.page_size = d.page_size;
+      pp.list_stride = d.block_table_stride;
+      pp.chunk_pages = seg_pages;
+      pp.chunks = (d.block_table_stride + seg_pages - 1) / seg_pages;
+      pp.scale_log2 = dp.scale_log2;
+      if (launch_pages(pp, d.kv_dtype, s) != hipSuccess) return DORA_ERR_HIP;
+      if (ev && c0 == 0 && hipEventRecord(ev[1], s) != hipSuccess) return DORA_ERR_HIP;
+      if (pp.chunks > 1 && launch_pages_combine(pp, s) != hipSuccess) return DORA_ERR_HIP;
+      continue;
+    }
     if (seg_pages > 0) {
       SegmentParams sp;
       sp.q = dp.q;
@@ -380,7 +428,8 @@ dora_status enqueue_decode(const dora_decode_desc& d, const void* q, const void*
       if (sp.seg_chunks > 1 && launch_combine_chunks(sp, s) != hipSuccess) return DORA_ERR_HIP;
       continue;
     }
-    if (launch_decode(dp, d.head_dim, d.page_size, fp8, w.waves, s) != hipSuccess)
+    if ((fp4 ? launch_decode4(dp, d.head_dim, d.page_size, w.waves, s)
+             : launch_decode(dp, d.head_dim, d.page_size, fp8, w.waves, s)) != hipSuccess)
       return DORA_ERR_HIP;
     if (ev && c0 == 0 && hipEventRecord(ev[1], s) != hipSuccess) return DORA_ERR_HIP;
     CombineParams cp{};
@@ -553,6 +602,26 @@ dora_status dora_kv_append(const dora_decode_desc* desc, const void* k_new, cons
   if (validate && d.page_owner && !version_ids) return DORA_ERR_INVALID_ARG;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages))
     return DORA_ERR_INVALID_ARG;
+  if (d.kv_dtype == DORA_KV_FP4) {
+    PathParams p{};
+    p.k_new = (const uint16_t*)k_new;
+    p.v_new = (const uint16_t*)v_new;
+    p.block_table = block_table;
+    p.seq_lens = seq_lens;
+    p.version_ids = validate ? version_ids : nullptr;
+    p.page_owner = validate ? d.page_owner : nullptr;
+    p.k_pages = (uint8_t*)k_pages;
+    p.v_pages = (uint8_t*)v_pages;
+    p.dev_status = dev_status;
+    p.num_seqs = d.num_seqs;
+    p.num_tokens = 1;
+    p.num_kv_heads = d.num_kv_heads;
+    p.head_dim = d.head_dim;
+    p.page_size = d.page_size;
+    p.stride = d.block_table_stride;
+    p.num_pages = d.num_pages;
+    return launch_append4(p, true, (hipStream_t)stream) == hipSuccess ? DORA_OK : DORA_ERR_HIP;
+  }
   AppendParams p;
   p.k_new = (const uint16_t*)k_new;
   p.v_new = (const uint16_t*)v_new;
@@ -586,10 +655,10 @@ dora_status check_pack_desc(const dora_pack_desc* d) {
   if (!d) return DORA_ERR_INVALID_ARG;
   if (d->num_kv_heads < 1 || d->page_size < 1 || d->head_dim < 1 || d->num_pages < 1)
     return DORA_ERR_INVALID_ARG;
-  if (d->kv_dtype != DORA_KV_BF16 && d->kv_dtype != DORA_KV_FP8_E4M3)
-    return DORA_ERR_UNSUPPORTED;
-  const int e = d->kv_dtype == DORA_KV_BF16 ? 2 : 1;
-  if (((int64_t)d->num_kv_heads * d->page_size * d->head_dim * e) % 16 != 0)
+  if (!kv_dtype_known(d->kv_dtype)) return DORA_ERR_UNSUPPORTED;
+  if (d->kv_dtype == DORA_KV_FP4 && (d->page_size % 16 != 0 || d->head_dim % 64 != 0))
+    return DORA_ERR_UNSUPPORTED;  // a tile's blocks are whole
+  if (kv_page_bytes(d->kv_dtype, d->num_kv_heads, d->page_size, d->head_dim) % 16 != 0)
     return DORA_ERR_UNSUPPORTED;
   return DORA_OK;
 }
@@ -600,8 +669,8 @@ extern "C" {
 
 size_t dora_kv_packed_bytes(const dora_pack_desc* desc, int64_t n_pages) {
   if (check_pack_desc(desc) != DORA_OK || n_pages < 0) return 0;
-  const int e = desc->kv_dtype == DORA_KV_BF16 ? 2 : 1;
-  const int64_t pb = (int64_t)desc->num_kv_heads * desc->page_size * desc->head_dim * e;
+  const int64_t pb =
+      kv_page_bytes(desc->kv_dtype, desc->num_kv_heads, desc->page_size, desc->head_dim);
   size_t total = 256 + (size_t)(2 * n_pages * pb);
   if (desc->kv_dtype == DORA_KV_FP8_E4M3) total += (size_t)(2 * n_pages * 4);
   return total;
@@ -629,7 +698,7 @@ dora_status dora_kv_page_pack(const dora_pack_desc* desc, const void* k_pages,
   p.pages = src_pages;
   p.n_pages = n_pages;
   p.num_pages = desc->num_pages;
-  p.page_bytes = (int64_t)desc->num_kv_heads * desc->page_size * desc->head_dim * (fp8 ? 1 : 2);
+  p.page_bytes = kv_page_bytes(desc->kv_dtype, desc->num_kv_heads, desc->page_size, desc->head_dim);
   p.packed = (uint8_t*)packed;
   p.has_scales = fp8 ? 1 : 0;
   make_pack_header(*desc, n_pages, &p.hdr);
@@ -656,7 +725,7 @@ dora_status dora_kv_page_unpack(const dora_pack_desc* desc, int32_t src_version,
   p.pages = dst_pages;
   p.n_pages = n_pages;
   p.num_pages = desc->num_pages;
-  p.page_bytes = (int64_t)desc->num_kv_heads * desc->page_size * desc->head_dim * (fp8 ? 1 : 2);
+  p.page_bytes = kv_page_bytes(desc->kv_dtype, desc->num_kv_heads, desc->page_size, desc->head_dim);
   p.packed_in = (const uint8_t*)packed;
   p.k_out = (uint8_t*)k_pages;
   p.v_out = (uint8_t*)v_pages;

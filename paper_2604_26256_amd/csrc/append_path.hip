@@ -24,6 +24,7 @@
 
 #include "cache_internal.h"
 #include "fp8_core.h"
+#include "path_core.h"
 
 namespace dora {
 
@@ -32,55 +33,6 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPathMaxThreads = 512;
-constexpr int kPathMaxPage = 32;  // tokens of a page, at most
-
-// The page that workgroup (b, k) writes: its id (-1: none, or it may not be written,
-// then reported), its slots [lo, hi), and for thread i < hi - lo the source row of slot lo + i.
-struct PathPage {
-  int64_t id;
-  int lo, hi, row;
-};
-
-__device__ __forceinline__ PathPage path_page(const PathParams& p, int b, int k) {
-  PathPage r{-1, 0, 0, 0};
-  const int P = p.page_size, L = p.seq_lens[b];
-  const int n = p.counts ? p.counts[b] : p.num_tokens;
-  if (n == 0) return r;
-  bool ok = n > 0 && n <= p.num_tokens && n <= L && (int64_t)L <= (int64_t)p.stride * P;
-  if (ok) {
-    const int base = L - n, j = base / P + k, t0 = j * P;
-    if (t0 >= L) return r;  // no such page
-    r.lo = base > t0 ? base - t0 : 0;
-    r.hi = L - t0 < P ? L - t0 : P;
-    const int i = t0 + r.lo - base + threadIdx.x;  // the token's place in the sequence's list
-    r.row = i;  // (loaded beside the page's id, which path_rows waits for)
-    if (p.path && (int)threadIdx.x < r.hi - r.lo) r.row = p.path[(int64_t)b * p.num_tokens + i];
-    r.id = p.block_table[(int64_t)b * p.stride + j];
-    ok = r.id >= 0 && r.id < p.num_pages;
-    if (ok && p.page_owner && p.version_ids) ok = p.page_owner[r.id] == p.version_ids[b];
-  }
-  if (!ok) {
-    if (threadIdx.x == 0 && p.dev_status) *p.dev_status = (int32_t)DORA_ERR_DEVICE_CHECK;
-    r.id = -1;
-  }
-  return r;
-}
-
-// The source rows of the page's tokens, into s_row; false (for all threads) where one is
-// no row: the page is skipped, and reported.
-__device__ __forceinline__ bool path_rows(const PathParams& p, const PathPage& pg, int* s_row,
-                                          int* s_bad) {
-  if (threadIdx.x < 64) {
-    const bool mine = (int)threadIdx.x < pg.hi - pg.lo;
-    if (mine) s_row[threadIdx.x] = pg.row;
-    const bool bad = __any(mine && (pg.row < 0 || pg.row >= p.num_tokens));
-    if (threadIdx.x == 0) *s_bad = bad;
-  }
-  __syncthreads();
-  if (!*s_bad) return true;
-  if (threadIdx.x == 0 && p.dev_status) *p.dev_status = (int32_t)DORA_ERR_DEVICE_CHECK;
-  return false;
-}
 
 // bf16.  K: a thread stores one 16-byte chunk of one token, neighbours the slots of a
 // chunk, non-temporally.  V: a thread takes 8 head-dim rows and 8 slots, turns them round

@@ -2,9 +2,9 @@
 // append, page copies.  Argument validation (before any launch, no side effects),
 // workspace layouts, launches.
 #include <hip/hip_runtime.h>
-#include <math.h>
 #include <stdint.h>
 
+#include "api_checks.h"
 #include "cache_internal.h"
 #include "cache_rules.h"
 
@@ -12,50 +12,15 @@ using namespace dora;
 
 namespace {
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-int compute_units() {
-  int dev = 0, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
-      cus <= 0) {
-    (void)hipGetLastError();  // no device here: size for a 256-CU part
-    cus = 256;
-  }
-  return cus;
+// (neither attention is built for 4-bit pages)
+dora_status check_nodes(const dora_decode_desc& d, int32_t num_nodes) {
+  if (num_nodes < 1 || num_nodes > 64) return DORA_ERR_INVALID_ARG;
+  return d.kv_dtype == DORA_KV_FP4 ? DORA_ERR_UNSUPPORTED : DORA_OK;
 }
 
-// The checks that both attention calls share, on a valid descriptor.
-dora_status check_attn(const dora_decode_desc& d, const void* q, const void* k_pages,
-                       const void* v_pages, const int32_t* block_table, const int32_t* seq_lens,
-                       const int32_t* version_ids, const void* out, const void* workspace) {
-  if (!q || !k_pages || !v_pages || !block_table || !seq_lens || !out || !workspace)
-    return DORA_ERR_INVALID_ARG;
-  if (d.kv_dtype == DORA_KV_FP8_E4M3 && (!d.k_scales || !d.v_scales)) return DORA_ERR_INVALID_ARG;
-  if ((d.flags & DORA_FLAG_VALIDATE) && !version_ids && d.page_owner) return DORA_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) ||
-      !aligned16(workspace))
-    return DORA_ERR_INVALID_ARG;
-  return DORA_OK;
-}
-
-float scale_log2_of(const dora_decode_desc& d) {
-  const float scale = d.sm_scale > 0.f ? d.sm_scale : 1.0f / sqrtf((float)d.head_dim);
-  // (the kernels take it for positive)
-  return fmaxf(scale * 1.4426950408889634f, 1e-30f);
-}
-
-int64_t page_bytes_of(const dora_decode_desc& d) {
-  return (int64_t)d.num_kv_heads * d.page_size * d.head_dim *
-         (d.kv_dtype == DORA_KV_FP8_E4M3 ? 1 : 2);
-}
-
-dora_status check_nodes(int32_t num_nodes) {
-  return num_nodes < 1 || num_nodes > 64 ? DORA_ERR_INVALID_ARG : DORA_OK;
-}
-
-dora_status check_window(int32_t window, int32_t sinks) {
-  return window < 1 || sinks < 0 ? DORA_ERR_INVALID_ARG : DORA_OK;
+dora_status check_window(const dora_decode_desc& d, int32_t window, int32_t sinks) {
+  if (window < 1 || sinks < 0) return DORA_ERR_INVALID_ARG;
+  return d.kv_dtype == DORA_KV_FP4 ? DORA_ERR_UNSUPPORTED : DORA_OK;
 }
 
 dora_status validate_window(const dora_decode_desc& d, const int32_t* block_table,
@@ -77,7 +42,7 @@ dora_status validate_window(const dora_decode_desc& d, const int32_t* block_tabl
 extern "C" {
 
 size_t dora_decode_tree_workspace_bytes(const dora_decode_desc* desc, int32_t num_nodes) {
-  if (check_desc(desc) != DORA_OK || check_nodes(num_nodes) != DORA_OK) return 0;
+  if (check_desc(desc) != DORA_OK || check_nodes(*desc, num_nodes) != DORA_OK) return 0;
   TreeLayout t;
   tree_layout(*desc, num_nodes, compute_units(), &t);
   return t.total;
@@ -93,7 +58,7 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
   dora_status st = check_desc(desc);
   if (st != DORA_OK) return st;
   const dora_decode_desc& d = *desc;
-  st = check_nodes(num_nodes);
+  st = check_nodes(d, num_nodes);
   if (st != DORA_OK) return st;
   if (d.num_seqs == 0) return DORA_OK;
   st = check_attn(d, q, k_pages, v_pages, block_table, seq_lens, version_ids, out, workspace);
@@ -153,7 +118,7 @@ dora_status dora_decode_attn_tree(const dora_decode_desc* desc, int32_t num_node
 
 size_t dora_decode_window_workspace_bytes(const dora_decode_desc* desc, int32_t window,
                                           int32_t sinks) {
-  if (check_desc(desc) != DORA_OK || check_window(window, sinks) != DORA_OK) return 0;
+  if (check_desc(desc) != DORA_OK || check_window(*desc, window, sinks) != DORA_OK) return 0;
   WindowLayout w;
   window_layout(*desc, window, sinks, &w);
   return w.total;
@@ -167,7 +132,7 @@ dora_status dora_decode_attn_window(const dora_decode_desc* desc, int32_t window
   dora_status st = check_desc(desc);
   if (st != DORA_OK) return st;
   const dora_decode_desc& d = *desc;
-  st = check_window(window, sinks);
+  st = check_window(d, window, sinks);
   if (st != DORA_OK) return st;
   if (d.num_seqs == 0) return DORA_OK;
   st = check_attn(d, q, k_pages, v_pages, block_table, seq_lens, version_ids, out, workspace);
@@ -253,7 +218,9 @@ dora_status dora_kv_append_path(const dora_decode_desc* desc, int32_t num_tokens
   p.page_size = d.page_size;
   p.stride = d.block_table_stride;
   p.num_pages = d.num_pages;
-  return launch_append_path(p, fp8, (hipStream_t)stream) == hipSuccess ? DORA_OK : DORA_ERR_HIP;
+  const hipError_t e = d.kv_dtype == DORA_KV_FP4 ? launch_append4(p, false, (hipStream_t)stream)
+                                                 : launch_append_path(p, fp8, (hipStream_t)stream);
+  return e == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }
 
 dora_status dora_kv_page_copy(const dora_pack_desc* desc, void* k_pages, void* v_pages,
@@ -279,7 +246,7 @@ dora_status dora_kv_page_copy(const dora_pack_desc* desc, void* k_pages, void* v
   p.dev_status = dev_status;
   p.n_pages = n_pages;
   p.num_pages = desc->num_pages;
-  p.page_bytes = (int64_t)desc->num_kv_heads * desc->page_size * desc->head_dim * (fp8 ? 1 : 2);
+  p.page_bytes = kv_page_bytes(desc->kv_dtype, desc->num_kv_heads, desc->page_size, desc->head_dim);
   p.has_scales = fp8 ? 1 : 0;
   p.layer = 0;
   return launch_page_copy(p, (hipStream_t)stream) == hipSuccess ? DORA_OK : DORA_ERR_HIP;

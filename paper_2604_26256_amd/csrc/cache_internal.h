@@ -117,6 +117,8 @@ struct PathParams {
   int64_t num_pages;
 };
 hipError_t launch_append_path(const PathParams& p, bool fp8, hipStream_t s);
+// 4-bit pages (append4.hip); single: one token of each sequence, as dora_kv_append takes it.
+hipError_t launch_append4(const PathParams& p, bool single, hipStream_t s);
 
 // Page copies.
 struct CopyParams {

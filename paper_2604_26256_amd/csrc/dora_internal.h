@@ -14,6 +14,7 @@ namespace dora {
 // never more than the resident slots).  One equal range per wavefront.
 constexpr int kBf16WavesPerCu = 4;
 constexpr int kFp8WavesPerCu = 7;
+constexpr int kFp4WavesPerCu = 8;
 // Smallest range (page-heads) a wavefront gets by default: a range must carry
 // enough bytes to amortise the wavefront's start-up (page prefix, first loads).
 constexpr int kMinRangePages = 8;
@@ -38,6 +39,15 @@ struct WsLayout {
 // (desc->num_waves if set).  Falls back to a 256-CU, 8-wave estimate when no
 // device can be queried.
 int64_t decode_waves(const dora_decode_desc& d);
+inline bool kv_dtype_known(int32_t t) {
+  return t == DORA_KV_BF16 || t == DORA_KV_FP8_E4M3 || t == DORA_KV_FP4;
+}
+// Bytes of one page of K (or of V), all KV heads.
+__host__ __device__ inline int64_t kv_page_bytes(int32_t kv_dtype, int64_t num_kv_heads, int64_t page_size,
+                             int64_t head_dim) {
+  const int64_t n = num_kv_heads * page_size * head_dim;
+  return kv_dtype == DORA_KV_BF16 ? 2 * n : kv_dtype == DORA_KV_FP8_E4M3 ? n : n / 32 * 17;
+}
 // Host-checkable validity of a descriptor.
 dora_status check_desc(const dora_decode_desc* d);
 dora_status check_pack_desc(const dora_pack_desc* d);
@@ -201,6 +211,11 @@ size_t decode_lds_bytes(int num_seqs);
 hipError_t decode_waves_per_cu(int head_dim, int page_size, bool fp8, int num_seqs, int* out);
 hipError_t launch_decode(const DecodeParams& p, int head_dim, int page_size, bool fp8,
                          int64_t waves, hipStream_t s);
+// The stream-K decode of 4-bit pages (decode4.hip): DecodeParams' records and partials, its
+// work counted in steps of 64 tokens.
+hipError_t decode4_waves_per_cu(int head_dim, int page_size, int num_seqs, int* out);
+hipError_t launch_decode4(const DecodeParams& p, int head_dim, int page_size, int64_t waves,
+                          hipStream_t s);
 hipError_t launch_segments(const SegmentParams& p, bool fp8, hipStream_t s);
 hipError_t launch_combine_chunks(const SegmentParams& p, hipStream_t s);
 hipError_t launch_combine(const CombineParams& p, int64_t waves, hipStream_t s);

@@ -31,8 +31,7 @@ constexpr int kGridPages = 32768;  // pages per grid layer, at most
 
 void make_pack_header(const dora_pack_desc& d, int64_t n_pages, PackHeader* h) {
   memset(h, 0, sizeof *h);
-  const int e = d.kv_dtype == DORA_KV_BF16 ? 2 : 1;
-  const int64_t page_bytes = (int64_t)d.num_kv_heads * d.page_size * d.head_dim * e;
+  const int64_t page_bytes = kv_page_bytes(d.kv_dtype, d.num_kv_heads, d.page_size, d.head_dim);
   uint8_t* p = (uint8_t*)h->words;
   memcpy(p + 0, "DORAKV01", 8);
   int32_t v32;

@@ -1,0 +1,96 @@
+// Internal declarations of attention over listed pages, the choice of pages and their
+// bounds, and reads of the cache.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "cache_internal.h"
+#include "dora.h"
+#include "dora_internal.h"
+
+namespace dora {
+
+// Attention over listed pages.
+struct PagesParams {
+  const uint16_t* q;
+  const uint8_t* k_pages;
+  const uint8_t* v_pages;
+  const float* k_scales;
+  const float* v_scales;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  const int32_t* lists;   // [B][Hkv][list_stride], or null: all pages of a row
+  const int32_t* counts;  // [B][Hkv]
+  uint16_t* out;
+  float* part_o;          // [segments * chunks][G][d] unnormalised partials
+  float2* part_ml;        // {max (log2 units), sum}; max -inf: nothing attended
+  int64_t page_bytes;
+  int32_t num_seqs, num_q_heads, num_kv_heads, group, stride, head_dim, page_size;
+  int32_t list_stride;
+  int32_t chunk_pages;    // listed pages of a workgroup
+  int32_t chunks;         // workgroups of a segment
+  float scale_log2;
+};
+hipError_t launch_pages(const PagesParams& p, int kv_dtype, hipStream_t s);
+hipError_t launch_pages_combine(const PagesParams& p, hipStream_t s);
+hipError_t launch_pages_validate(const ValidateParams& p, const int32_t* lists, const int32_t* counts,
+                                 int num_kv_heads, int list_stride, hipStream_t s);
+
+// Listed pages that a workgroup stages in LDS, at most.
+constexpr int kPagesMaxChunk = 512;
+
+struct PagesLayout {
+  int chunk_pages, chunks;
+  size_t part_o_off, part_ml_off, total;
+};
+
+// Listed pages of a workgroup, and what the workspace holds.
+inline void pages_layout(const dora_decode_desc& d, int32_t list_stride, PagesLayout* w) {
+  const int seqs = d.num_seqs < kMaxSeqsPerLaunch ? d.num_seqs : kMaxSeqsPerLaunch;
+  const int64_t segs = (int64_t)seqs * d.num_kv_heads;
+  int64_t chunk = segs > 0 ? (list_stride * segs + 1023) / 1024 : list_stride;
+  const int64_t least = 256 / d.page_size;
+  chunk = (chunk + least - 1) / least * least;
+  if (chunk > kPagesMaxChunk) chunk = kPagesMaxChunk;
+  if (chunk > list_stride) chunk = list_stride;
+  w->chunk_pages = (int)chunk;
+  w->chunks = (int)((list_stride + chunk - 1) / chunk);
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  const size_t slots = w->chunks > 1 ? (size_t)segs * w->chunks : 0;
+  const size_t G = (size_t)(d.num_q_heads / d.num_kv_heads);
+  w->part_o_off = kWsHeaderBytes;
+  w->part_ml_off = up(w->part_o_off + slots * G * d.head_dim * 4);
+  w->total = up(w->part_ml_off + slots * G * 8);
+}
+
+// Bytes of a page's bounds: int8 [Hkv][2][d] (largest, smallest), fp32 [Hkv] scales.
+__host__ __device__ inline int64_t bounds_bytes(int64_t num_kv_heads, int64_t head_dim) {
+  return (num_kv_heads * (2 * head_dim + 4) + 15) / 16 * 16;
+}
+// Bounds of the pages that the last tokens lie in (k_pages and k_scales are read).
+hipError_t launch_page_bounds(const PathParams& p, const float* k_scales, uint8_t* bounds,
+                              int kv_dtype, hipStream_t s);
+
+struct SelectParams {
+  const uint16_t* q;
+  const uint8_t* bounds;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  float* scores;          // [B][Hkv][stride]
+  int32_t* lists;         // [B][Hkv][budget]
+  int32_t* counts;        // [B][Hkv]
+  int64_t record;         // bytes of a page's bounds
+  int32_t num_seqs, num_q_heads, num_kv_heads, group, stride, head_dim, page_size;
+  int32_t budget, sinks, recent;
+  int32_t chunk_pages;    // pages of a scoring workgroup
+};
+hipError_t launch_page_scores(const SelectParams& p, hipStream_t s);
+hipError_t launch_page_select(const SelectParams& p, hipStream_t s);
+
+// Rows of the last tokens, as bf16 (PathParams' k_new, v_new and path are not used).
+hipError_t launch_kv_read(const PathParams& p, const float* k_scales, const float* v_scales,
+                          uint16_t* k_out, uint16_t* v_out, int kv_dtype, hipStream_t s);
+
+}  // namespace dora

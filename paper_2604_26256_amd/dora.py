@@ -32,6 +32,7 @@ DORA_ERR_NOT_FOUND = 8
 
 DORA_KV_BF16 = 0
 DORA_KV_FP8_E4M3 = 1
+DORA_KV_FP4 = 4
 DORA_FLAG_VALIDATE = 0x1
 
 
@@ -106,6 +107,21 @@ _lib.dora_decode_attn_window.restype = ctypes.c_int
 _lib.dora_kv_append_path.argtypes = [_DescP, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                      _P]
 _lib.dora_kv_append_path.restype = ctypes.c_int
+_lib.dora_kv_read.argtypes = [_DescP, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]
+_lib.dora_kv_read.restype = ctypes.c_int
+_lib.dora_page_bounds_bytes.argtypes = [_I32, _I32]
+_lib.dora_page_bounds_bytes.restype = _SZ
+_lib.dora_kv_page_bounds.argtypes = [_DescP, _I32, _P, _P, _P, _P, _P, _P, _P, _P]
+_lib.dora_kv_page_bounds.restype = ctypes.c_int
+_lib.dora_page_select_workspace_bytes.argtypes = [_DescP]
+_lib.dora_page_select_workspace_bytes.restype = _SZ
+_lib.dora_page_select.argtypes = [_DescP, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ,
+                                  _P]
+_lib.dora_page_select.restype = ctypes.c_int
+_lib.dora_decode_pages_workspace_bytes.argtypes = [_DescP, _I32]
+_lib.dora_decode_pages_workspace_bytes.restype = _SZ
+_lib.dora_decode_attn_pages.argtypes = [_DescP, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+_lib.dora_decode_attn_pages.restype = ctypes.c_int
 _lib.dora_plan_partition.argtypes = [ctypes.POINTER(_I64), _I32, _I32, ctypes.POINTER(_I32)]
 _lib.dora_plan_partition.restype = ctypes.c_int
 _lib.dora_plan_supplement.argtypes = [ctypes.POINTER(_I32), ctypes.POINTER(_I32), _I32, _I32,
@@ -237,22 +253,32 @@ def _stream_handle(stream, device=None):
                                               else device.index)
 
 
-def _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, head_dim, kv_dtype):
+def _k_geometry(k_pages, num_kv_heads, page_size, head_dim, kv_dtype):
+    """Pages of a K pool of this shape, and the tensor types that hold it."""
     torch = _torch()
-    X = 16 // (2 if kv_dtype == DORA_KV_BF16 else 1)
-    if head_dim % X:
-        raise ValueError("head_dim must be a multiple of 16 bytes of elements")
-    kshape_tail = (num_kv_heads, head_dim // X, page_size, X)
-    vshape_tail = (num_kv_heads, head_dim, page_size)
-    if k_pages.shape[1:] != kshape_tail:
-        raise ValueError(f"k_pages must be [num_pages]{list(kshape_tail)}, got "
-                         f"{list(k_pages.shape)}")
-    if v_pages.shape[1:] != vshape_tail or v_pages.shape[0] != k_pages.shape[0]:
-        raise ValueError(f"v_pages must be [num_pages]{list(vshape_tail)}, got "
-                         f"{list(v_pages.shape)}")
-    kv_types = (torch.bfloat16,) if kv_dtype == DORA_KV_BF16 else (torch.uint8,
-                                                                   torch.float8_e4m3fn)
+    if kv_dtype == DORA_KV_FP4:
+        if head_dim % 64 or page_size % 16:
+            raise ValueError("4-bit pages: head_dim a multiple of 64, page_size of 16")
+        tail = (num_kv_heads, page_size * head_dim * 17 // 32)
+    else:
+        X = 16 // (2 if kv_dtype == DORA_KV_BF16 else 1)
+        if head_dim % X:
+            raise ValueError("head_dim must be a multiple of 16 bytes of elements")
+        tail = (num_kv_heads, head_dim // X, page_size, X)
+    if k_pages.shape[1:] != tail:
+        raise ValueError(f"k_pages must be [num_pages]{list(tail)}, got {list(k_pages.shape)}")
+    kv_types = ((torch.bfloat16,) if kv_dtype == DORA_KV_BF16 else (torch.uint8,)
+                if kv_dtype == DORA_KV_FP4 else (torch.uint8, torch.float8_e4m3fn))
     return int(k_pages.shape[0]), kv_types
+
+
+def _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, head_dim, kv_dtype):
+    num_pages, kv_types = _k_geometry(k_pages, num_kv_heads, page_size, head_dim, kv_dtype)
+    tail = (tuple(k_pages.shape[1:]) if kv_dtype == DORA_KV_FP4
+            else (num_kv_heads, head_dim, page_size))
+    if v_pages.shape[1:] != tail or v_pages.shape[0] != num_pages:
+        raise ValueError(f"v_pages must be [num_pages]{list(tail)}, got {list(v_pages.shape)}")
+    return num_pages, kv_types
 
 
 def make_decode_desc(*, num_seqs, num_q_heads, num_kv_heads, head_dim, page_size,
@@ -861,6 +887,192 @@ def dora_kv_page_copy(k_pages, v_pages, src_pages, dst_pages, *, num_kv_heads, p
     scales = ptrs[5:7] if k_scales is not None else (None, None)
     _call(k_pages.device, stream, "dora_kv_page_copy",
           (ctypes.byref(desc), *ptrs[:2], *scales, *ptrs[2:4], n, ptrs[4]))
+
+
+def _last_tokens(rows, num_kv_heads, page_size, head_dim, block_table, num_pages, kv_dtype,
+                 k_scales, v_scales, page_owner, flags):
+    """Descriptor of a call that goes by the last tokens of each of `rows` sequences."""
+    if block_table.dim() != 2 or block_table.shape[0] != rows:
+        raise ValueError("block_table must be [B][stride]")
+    return make_decode_desc(num_seqs=rows, num_q_heads=num_kv_heads, num_kv_heads=num_kv_heads,
+                            head_dim=head_dim, page_size=page_size,
+                            block_table_stride=max(1, block_table.shape[1]), num_pages=num_pages,
+                            kv_dtype=kv_dtype, k_scales=k_scales, v_scales=v_scales,
+                            page_owner=page_owner, flags=flags)
+
+
+def dora_kv_read(k_pages, v_pages, block_table, seq_lens, k_out, v_out, *, num_kv_heads, page_size,
+                 counts=None, kv_dtype=DORA_KV_BF16, k_scales=None, v_scales=None, version_ids=None,
+                 page_owner=None, flags=0, dev_status=None, stream=None):
+    """Read the last counts[b] (T without counts) tokens of each sequence into rows of k_out and
+    v_out (bf16 [B][T][Hkv][d]); see include/dora.h."""
+    torch = _torch()
+    if k_out.dim() != 4 or k_out.shape[2] != num_kv_heads:
+        raise ValueError("k_out must be [B][T][num_kv_heads][head_dim]")
+    B, T, _, D = k_out.shape
+    num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
+    if kv_dtype != DORA_KV_FP8_E4M3:
+        k_scales = v_scales = None
+    elif B:
+        _need(k_scales=k_scales, v_scales=v_scales)
+    desc = _last_tokens(B, num_kv_heads, page_size, D, block_table, num_pages, kv_dtype,
+                        k_scales, v_scales, page_owner, flags)
+    if B == 0:
+        return
+    _need(seq_lens=seq_lens, v_out=v_out)
+    _one_status(dev_status)
+    bf16, i32, rows = (torch.bfloat16,), (torch.int32,), (B,)
+    ptrs = _marshal(k_out.device, stream, [
+        (counts, "counts", i32, rows, 4),
+        (k_pages, "k_pages", kv_types, None, 16),
+        (v_pages, "v_pages", kv_types, None, 16),
+        (block_table, "block_table", i32, None, 4),
+        (seq_lens, "seq_lens", i32, rows, 4),
+        (version_ids, "version_ids", i32, rows, 4),
+        (k_out, "k_out", bf16, None, 16),
+        (v_out, "v_out", bf16, k_out.shape, 16),
+        (dev_status, "dev_status", i32, None, 4),
+        *_scale_specs(k_scales, v_scales, page_owner, num_pages)])
+    _call(k_out.device, stream, "dora_kv_read", (ctypes.byref(desc), T, *ptrs[:9]))
+
+
+def dora_page_bounds_bytes(num_kv_heads, head_dim) -> int:
+    """Bytes of one page's bounds (0 for an unsupported geometry)."""
+    return int(_lib.dora_page_bounds_bytes(_i32("num_kv_heads", num_kv_heads),
+                                           _i32("head_dim", head_dim)))
+
+
+def _bounds_shape(num_pages, num_kv_heads, head_dim):
+    return num_pages, dora_page_bounds_bytes(num_kv_heads, head_dim)
+
+
+def dora_kv_page_bounds(k_pages, block_table, seq_lens, bounds, *, num_tokens, head_dim, num_kv_heads,
+                        page_size, counts=None, kv_dtype=DORA_KV_BF16, k_scales=None, version_ids=None,
+                        page_owner=None, flags=0, dev_status=None, stream=None):
+    """Bounds (uint8 [num_pages][dora_page_bounds_bytes]) of the keys of every page that the last
+    counts[b] (num_tokens without counts) tokens of a sequence lie in; see include/dora.h."""
+    torch = _torch()
+    num_tokens = _i32("num_tokens", num_tokens)
+    B = seq_lens.shape[0]
+    num_pages, kv_types = _k_geometry(k_pages, num_kv_heads, page_size, head_dim, kv_dtype)
+    if kv_dtype != DORA_KV_FP8_E4M3:
+        k_scales = None
+    elif B:
+        _need(k_scales=k_scales)
+    desc = _last_tokens(B, num_kv_heads, page_size, head_dim, block_table,
+                        num_pages, kv_dtype, k_scales, None, page_owner, flags)
+    if B == 0:
+        return
+    _need(bounds=bounds)
+    _one_status(dev_status)
+    i32, rows = (torch.int32,), (B,)
+    ptrs = _marshal(k_pages.device, stream, [
+        (counts, "counts", i32, rows, 4),
+        (k_pages, "k_pages", kv_types, None, 16),
+        (block_table, "block_table", i32, None, 4),
+        (seq_lens, "seq_lens", i32, rows, 4),
+        (version_ids, "version_ids", i32, rows, 4),
+        (bounds, "bounds", (torch.uint8,), _bounds_shape(num_pages, num_kv_heads, head_dim), 16),
+        (dev_status, "dev_status", i32, None, 4),
+        *_scale_specs(k_scales, None, page_owner, num_pages)])
+    _call(k_pages.device, stream, "dora_kv_page_bounds", (ctypes.byref(desc), num_tokens, *ptrs[:7]))
+
+
+def dora_page_select_workspace_bytes(desc: dora_decode_desc) -> int:
+    """Workspace of dora_page_select without scores (0 on invalid arguments)."""
+    return int(_lib.dora_page_select_workspace_bytes(ctypes.byref(desc)))
+
+
+def dora_page_select(q, bounds, block_table, seq_lens, page_lists, page_counts, *, num_kv_heads,
+                     page_size, sink_pages=1, recent_pages=1, scores=None, version_ids=None,
+                     page_owner=None, flags=0, workspace=None, stream=None):
+    """Choose the pages that each sequence's KV heads read (see include/dora.h): page_lists (int32
+    [B][Hkv][budget]) receives their numbers, ascending, page_counts (int32 [B][Hkv]) how many; the
+    first sink_pages and the last recent_pages are always among them.  q: bf16 [B][Hq][d]; bounds:
+    as dora_kv_page_bounds writes them; scores: optional fp32 [B][Hkv][stride]."""
+    torch = _torch()
+    if q.dim() != 3:
+        raise ValueError("q must be [B][num_q_heads][head_dim]")
+    B, Hq, D = q.shape
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B][stride]")
+    if page_lists.dim() != 3:
+        raise ValueError("page_lists must be [B][num_kv_heads][budget]")
+    stride, budget = block_table.shape[1], page_lists.shape[2]
+    desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
+                            page_size=page_size, block_table_stride=max(1, stride),
+                            num_pages=bounds.shape[0], page_owner=page_owner, flags=flags)
+    if B == 0:
+        return
+    _need(seq_lens=seq_lens, page_counts=page_counts)
+    i32, rows, heads = (torch.int32,), (B,), (B, num_kv_heads)
+    ptrs = _marshal(q.device, stream, [
+        (q, "q", (torch.bfloat16,), None, 16),
+        (bounds, "bounds", (torch.uint8,), _bounds_shape(bounds.shape[0], num_kv_heads, D), 16),
+        (block_table, "block_table", i32, None, 4),
+        (seq_lens, "seq_lens", i32, rows, 4),
+        (version_ids, "version_ids", i32, rows, 4),
+        (page_lists, "page_lists", i32, (*heads, budget), 4),
+        (page_counts, "page_counts", i32, heads, 4),
+        (scores, "scores", (torch.float32,), (*heads, stride), 4),
+        *_scale_specs(None, None, page_owner, bounds.shape[0])])
+    _call_with_workspace(q.device, stream, "dora_page_select",
+                         (ctypes.byref(desc), budget, _i32("sink_pages", sink_pages),
+                          _i32("recent_pages", recent_pages), *ptrs[:8]),
+                         "dora_page_select_workspace_bytes", (), workspace)
+
+
+def dora_decode_pages_workspace_bytes(desc: dora_decode_desc, list_stride) -> int:
+    """Workspace of dora_decode_attn_pages (0 on invalid arguments)."""
+    return int(_lib.dora_decode_pages_workspace_bytes(ctypes.byref(desc),
+                                                      _i32("list_stride", list_stride)))
+
+
+def dora_decode_attn_pages(q, page_lists, page_counts, k_pages, v_pages, block_table, seq_lens,
+                           version_ids, out, *, num_kv_heads, page_size, kv_dtype=DORA_KV_BF16,
+                           sm_scale=0.0, k_scales=None, v_scales=None, page_owner=None, flags=0,
+                           workspace=None, stream=None):
+    """Decode attention over listed pages (see include/dora.h): page_lists int32
+    [B][Hkv][list_stride], numbers of a sequence's pages, of which page_counts int32 [B][Hkv]
+    are listed.  Other arguments as for dora_decode_attn.  Returns `out`."""
+    torch = _torch()
+    if q.dim() != 3:
+        raise ValueError("q must be [B][num_q_heads][head_dim]")
+    B, Hq, D = q.shape
+    num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B][stride]")
+    if page_lists.dim() != 3:
+        raise ValueError("page_lists must be [B][num_kv_heads][list_stride]")
+    if kv_dtype != DORA_KV_FP8_E4M3:
+        k_scales = v_scales = None
+    elif B:
+        _need(k_scales=k_scales, v_scales=v_scales)
+    desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
+                            page_size=page_size, block_table_stride=max(1, block_table.shape[1]),
+                            num_pages=num_pages, kv_dtype=kv_dtype, sm_scale=sm_scale,
+                            k_scales=k_scales, v_scales=v_scales, page_owner=page_owner,
+                            flags=flags)
+    if B == 0:
+        return out
+    _need(page_counts=page_counts, seq_lens=seq_lens, out=out)
+    width = page_lists.shape[2]
+    bf16, i32, rows, heads = (torch.bfloat16,), (torch.int32,), (B,), (B, num_kv_heads)
+    ptrs = _marshal(q.device, stream, [
+        (q, "q", bf16, None, 16),
+        (page_lists, "page_lists", i32, (*heads, width), 4),
+        (page_counts, "page_counts", i32, heads, 4),
+        (k_pages, "k_pages", kv_types, None, 16),
+        (v_pages, "v_pages", kv_types, None, 16),
+        (block_table, "block_table", i32, None, 4),
+        (seq_lens, "seq_lens", i32, rows, 4),
+        (version_ids, "version_ids", i32, rows, 4),
+        (out, "out", bf16, (B, Hq, D), 16),
+        *_scale_specs(k_scales, v_scales, page_owner, num_pages)])
+    _call_with_workspace(q.device, stream, "dora_decode_attn_pages",
+                         (ctypes.byref(desc), width, *ptrs[:9]),
+                         "dora_decode_pages_workspace_bytes", (width,), workspace)
+    return out
 
 
 def plan_partition(workload, n_groups):

@@ -155,23 +155,19 @@ __global__ __launch_bounds__(64, 2) void decode4_kernel(DecodeParams p) {
   typename F::Regs buf[2];
   load_ids(ids, kid, vid);
   load_pages(page, buf[0], kid, vid);
-  if (x0 + 1 < x1) {
-    next(ids);
-    load_ids(ids, kid, vid);
-  }
+  if (x0 + 1 < x1) next(ids);
+  load_ids(ids, kid, vid);
   int x = x0;
   while (true) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      if (x + 1 < x1) {  // uniform
-        next(page);
-        const int k = kid, v = vid;
-        if (x + 2 < x1) {
-          next(ids);
-          load_ids(ids, kid, vid);
-        }
-        load_pages(page, buf[r ^ 1], k, v);
-      }
+      // Behind the range's end the loads are made again: under a branch they would be waited for
+      // together with those before them.
+      const int k = kid, v = vid;
+      if (x + 1 < x1) next(page);
+      if (x + 2 < x1) next(ids);
+      load_ids(ids, kid, vid);
+      load_pages(page, buf[r ^ 1], k, v);
       if (x == x0 || here.u == 0) {
         whole = begun_here = here.u == 0;
         m_run = kNoMax;

@@ -209,8 +209,8 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void pages4_kernel(PagesParams p
     typename F::Regs buf[2];
     int nv[2];
     auto prefetch = [&](int r, int u) {
-      if (u >= steps) return;  // uniform
-      const int i = F::PAGES * (wave + kSegWaves * u), last = n - 1;
+      // (past the last step it is loaded again: under a branch the loads would be waited for together)
+      const int i = F::PAGES * (wave + kSegWaves * (u < steps ? u : steps - 1)), last = n - 1;
       const int ik = i + F::k_page(lane), iv = i + F::v_page(lane);  // past the end: no tokens
       const int64_t k = s.stage.id[ik < n ? ik : last], v = s.stage.id[iv < n ? iv : last];
       nv[r] = iv < n ? s.stage.tokens[iv] - F::group_slot(lane) : 0;

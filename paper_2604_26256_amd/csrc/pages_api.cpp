@@ -212,8 +212,7 @@ dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32
   p.budget = budget;
   p.sinks = sink_pages;
   p.recent = recent_pages;
-  p.chunk_pages = 256;
-  if (launch_page_scores(p, s) != hipSuccess) return DORA_ERR_HIP;
+  if (launch_page_scores(p, compute_units(), s) != hipSuccess) return DORA_ERR_HIP;
   return launch_page_select(p, s) == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }
 

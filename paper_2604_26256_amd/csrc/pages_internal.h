@@ -84,9 +84,8 @@ struct SelectParams {
   int64_t record;         // bytes of a page's bounds
   int32_t num_seqs, num_q_heads, num_kv_heads, group, stride, head_dim, page_size;
   int32_t budget, sinks, recent;
-  int32_t chunk_pages;    // pages of a scoring workgroup
 };
-hipError_t launch_page_scores(const SelectParams& p, hipStream_t s);
+hipError_t launch_page_scores(const SelectParams& p, int cus, hipStream_t s);
 hipError_t launch_page_select(const SelectParams& p, hipStream_t s);
 
 // Rows of the last tokens, as bf16 (PathParams' k_new, v_new and path are not used).

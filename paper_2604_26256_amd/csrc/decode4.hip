@@ -19,7 +19,7 @@ __device__ __forceinline__ int steps4_of(int L, int P, int stride) {
   return (int)(((int64_t)n + kFp4Step - 1) / kFp4Step);
 }
 
-template <int D, int P>
+template <int D, int P, int NBUF>
 __global__ __launch_bounds__(64, 2) void decode4_kernel(DecodeParams p) {
   typedef Fp4<D, P> F;
   constexpr int DBLK = D / 16;
@@ -73,9 +73,12 @@ __global__ __launch_bounds__(64, 2) void decode4_kernel(DecodeParams p) {
   struct Place {
     int b, g, u, n, L;
   };
+  // (by scalar loads: a vector load would be waited for together with the pages under way)
+  typedef __attribute__((address_space(4))) const int32_t constant_i32;
+  constant_i32* lens = (constant_i32*)(uintptr_t)p.seq_lens;
   auto at_sequence = [&](Place& c) {
     c.n = uni(sN[c.b + 1] - sN[c.b]);
-    c.L = uni(p.seq_lens[c.b]);
+    c.L = lens[c.b];
     const int64_t most = (int64_t)p.stride * P;
     if (c.L > most) c.L = (int)most;
   };
@@ -84,7 +87,7 @@ __global__ __launch_bounds__(64, 2) void decode4_kernel(DecodeParams p) {
     c.u = 0;
     if (++c.g < Hkv) return;
     c.g = 0;
-    do ++c.b; while (c.b < B && sN[c.b + 1] == sN[c.b]);
+    do ++c.b; while (c.b < B && uni(sN[c.b + 1] - sN[c.b]) == 0);
     if (c.b < B) at_sequence(c);
   };
   Place ids, page, here;  // of the next ids, the next pages, the step that is consumed
@@ -152,22 +155,30 @@ __global__ __launch_bounds__(64, 2) void decode4_kernel(DecodeParams p) {
     first_seg = false;
   };
 
-  typename F::Regs buf[2];
+  // The ids of a step are loaded one step before its pages, the pages NBUF - 1 steps before they are used.  Behind the
+  // range's end the loads are made again: under a branch they would be waited for with those before them; for the
+  // same reason the loads before the loop come in the loop's order.
+  typename F::Regs buf[NBUF];
+  int left_ids = x1 - x0 - 1, left_pages = x1 - x0 - 1;  // steps that are behind `ids` and `page`
+  auto advance = [&](Place& c, int& left) {
+    if (left > 0) {
+      --left;
+      next(c);
+    }
+  };
   load_ids(ids, kid, vid);
-  load_pages(page, buf[0], kid, vid);
-  if (x0 + 1 < x1) next(ids);
-  load_ids(ids, kid, vid);
+#pragma unroll
+  for (int i = 0; i < NBUF - 1; ++i) {
+    const int k = kid, v = vid;
+    if (i > 0) advance(page, left_pages);
+    advance(ids, left_ids);
+    load_ids(ids, kid, vid);
+    load_pages(page, buf[i], k, v);
+  }
   int x = x0;
   while (true) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      // Behind the range's end the loads are made again: under a branch they would be waited for
-      // together with those before them.
-      const int k = kid, v = vid;
-      if (x + 1 < x1) next(page);
-      if (x + 2 < x1) next(ids);
-      load_ids(ids, kid, vid);
-      load_pages(page, buf[r ^ 1], k, v);
+    for (int r = 0; r < NBUF; ++r) {
       if (x == x0 || here.u == 0) {
         whole = begun_here = here.u == 0;
         m_run = kNoMax;
@@ -175,9 +186,18 @@ __global__ __launch_bounds__(64, 2) void decode4_kernel(DecodeParams p) {
 #pragma unroll
         for (int i = 0; i < DBLK; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         F::load_query(q, p.q + ((int64_t)here.b * Hq + (int64_t)here.g * G + col) * D, col < G);
+        // waited for here, before the next pages' loads: after the branch it would be with them
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) asm volatile("" : "+v"(q[i]));
       }
+      const int k = kid, v = vid;
+      advance(page, left_pages);
+      advance(ids, left_ids);
+      load_ids(ids, kid, vid);
+      load_pages(page, buf[(r + NBUF - 1) % NBUF], k, v);
       const int left = here.L - here.u * kFp4Step;
-      F::consume(buf[r], left >= kFp4Step, left - 16 * grp, p.scale_log2, q, acc, m_run, l_run);
+      F::consume(buf[r], left >= kFp4Step, left - 16 * grp, p.scale_log2, [&](int s) { return q[s]; }, acc,
+                 m_run, l_run);
       const bool last = here.u == here.n - 1;
       if (last || x == x1 - 1) {
         whole = whole && last;
@@ -193,8 +213,8 @@ done:
 
 static const void* decode4_symbol(int head_dim, int page_size) {
   if (head_dim == 128)
-    return page_size == 16 ? (const void*)&decode4_kernel<128, 16> : (const void*)&decode4_kernel<128, 32>;
-  return page_size == 16 ? (const void*)&decode4_kernel<64, 16> : (const void*)&decode4_kernel<64, 32>;
+    return page_size == 16 ? (const void*)&decode4_kernel<128, 16, 2> : (const void*)&decode4_kernel<128, 32, 2>;
+  return page_size == 16 ? (const void*)&decode4_kernel<64, 16, 2> : (const void*)&decode4_kernel<64, 32, 2>;
 }
 
 hipError_t decode4_waves_per_cu(int head_dim, int page_size, int num_seqs, int* out) {

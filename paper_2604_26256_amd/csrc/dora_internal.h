@@ -14,7 +14,7 @@ namespace dora {
 // never more than the resident slots).  One equal range per wavefront.
 constexpr int kBf16WavesPerCu = 4;
 constexpr int kFp8WavesPerCu = 7;
-constexpr int kFp4WavesPerCu = 8;
+constexpr int kFp4WavesPerCu = 4;
 // Smallest range (page-heads) a wavefront gets by default: a range must carry
 // enough bytes to amortise the wavefront's start-up (page prefix, first loads).
 constexpr int kMinRangePages = 8;

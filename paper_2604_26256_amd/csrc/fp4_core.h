@@ -62,7 +62,7 @@ struct Fp4 {
     return (uint32_t)((lane & 15) * (P / 2) + group_slot(lane) / 2);
   }
   static __device__ __forceinline__ uint32_t v_scale_off(int lane) {
-    return (uint32_t)(CODES + 2 * group_slot(lane));
+    return (uint32_t)(CODES + 2 * (group_slot(lane) + (lane & 15)));
   }
 
   typedef typename std::conditional<D == 128, u32x4, u32x2>::type kraw_t;
@@ -70,7 +70,7 @@ struct Fp4 {
     kraw_t k[4];          // D / 4 dims of a token, of each sub-tile
     uint32_t ks;          // their exponents, a byte each
     u32x2 v[D / 16];      // 16 tokens of a dim
-    u32x4 vs[D / 64][2];  // bf16 scales of 16 tokens
+    uint16_t vs[D / 64];  // bf16 scales of token `lane & 15` of the lane's row group
   };
 
   // kt, vt: the lane's tiles.
@@ -86,9 +86,7 @@ struct Fp4 {
       r.v[i] = __builtin_nontemporal_load((const u32x2*)(vt + voff + i * 8 * P));
 #pragma unroll
     for (int h = 0; h < D / 64; ++h)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        r.vs[h][i] = __builtin_nontemporal_load((const u32x4*)(vt + vsoff + 2 * P * h + 16 * i));
+      r.vs[h] = __builtin_nontemporal_load((const uint16_t*)(vt + vsoff + 2 * P * h));
   }
 
   // The query operand: a lane's values are those of the dims that it holds of K.
@@ -108,60 +106,87 @@ struct Fp4 {
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   }
 
-  // The step: scores, online softmax in the log2 domain, weighted values.  nv: of the 16
-  // tokens of the lane's row group those that count, the first nv; `all`: every lane's do
-  // (uniform).  What the other slots hold is not used: a code is finite whatever it is, and
-  // scores and scaled weights are replaced.
-  static __device__ __forceinline__ void consume(const Regs& r, bool all, int nv, float mul,
-                                                 const Query& q, f32x4 (&acc)[D / 16],
-                                                 float& m_run, float& l_run) {
-    f32x4 sc[4];
+  // x times the value that lane U of the lane's row of 16 has in y.
+  template <int U>
+  static __device__ __forceinline__ float times_of(float x, float y) {
+    return x * __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x150 + U, 0xF, 0xF, true));
+  }
+  template <int U>
+  static __device__ __forceinline__ void scaled(bf16x8 (&w)[2], const f32x4 (&p)[4], float scale) {
+    if constexpr (U < 16) {
+      w[U >> 3][U & 7] = (__bf16)times_of<U>(p[U >> 2][U & 3], scale);
+      scaled<U + 1>(w, p, scale);
+    }
+  }
+
+  // The step: scores, softmax weights in the log2 domain, weighted values.  q(s): the query operand of
+  // k-step s.  nv: of the 16 tokens of the
+  // lane's row group those that count, the first nv; `all`: every lane's do (uniform).  What the other
+  // slots hold is not used: a code is finite whatever it is, and scores and scales are replaced.
+  //   m_run is a reference and not the running maximum: it moves only where a lane's weights sum to more than
+  // kMostWeight, so that most steps neither look for their maximum nor rescale.
+  static constexpr float kMostWeight = 256.f;
+  template <typename QueryAt>
+  static __device__ __forceinline__ void consume(const Regs& r, bool all, int nv, float mul, QueryAt q,
+                                                 f32x4 (&acc)[D / 16], float& m_run, float& l_run) {
+    f32x4 sc[4], p[4];
+    float ks[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const float scale = __uint_as_float(((r.ks >> (8 * t)) & 0xFFu) << 23);
+      ks[t] = __uint_as_float(((r.ks >> (8 * t)) & 0xFFu) << 23);
       sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s)
-        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(r.k[t][s], scale), q[s], sc[t], 0, 0, 0);
     }
-    float mx = -__builtin_inff();
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int s = 0; s < D / 32; ++s) {
+      const bf16x8 row = q(s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x = sc[t][i] * mul;
-        if (!all && 4 * t + i >= nv) x = -__builtin_inff();
-        sc[t][i] = x;
-        mx = fmaxf(mx, x);
-      }
-    mx = max_xor32(max_xor16(mx));
-    const float m_new = fmaxf(m_run, mx);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    m_run = m_new;
-    float sum = 0.f;
+      for (int t = 0; t < 4; ++t)
+        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(r.k[t][s], ks[t]), row, sc[t], 0, 0, 0);
+    }
+    float scale[D / 64];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int h = 0; h < D / 64; ++h) scale[h] = __uint_as_float((uint32_t)r.vs[h] << 16);
+    if (!all) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sc[t][i] = __builtin_amdgcn_exp2f(sc[t][i] - m_new);
-        sum += sc[t][i];
-      }
-    l_run = __builtin_fmaf(l_run, alpha, sum);
-    if (__ballot(alpha != 1.f)) {
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * t + i >= nv) sc[t][i] = -__builtin_inff();
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h)
+        if ((int)(threadIdx.x & 15) >= nv) scale[h] = 0.f;
+    }
+    float sum;
+    auto weigh = [&]() {
+      sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i], mul, -m_run));
+          sum += p[t][i];
+        }
+    };
+    weigh();
+    if (__ballot(!(sum <= kMostWeight))) {  // uniform
+      float mx = -__builtin_inff();
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[t][i]);
+      const float m_new = fmaxf(m_run, mul * max_xor32(max_xor16(mx)));
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) acc[i] *= alpha;
+      weigh();
     }
+    l_run += sum;
 #pragma unroll
     for (int h = 0; h < D / 64; ++h) {
       bf16x8 w[2];
-#pragma unroll
-      for (int u = 0; u < 16; ++u) {
-        const uint32_t two = r.vs[h][u >> 3][(u >> 1) & 3];
-        const float scale = __uint_as_float(u & 1 ? two & 0xFFFF0000u : two << 16);
-        float x = sc[u >> 2][u & 3] * scale;
-        if (!all && u >= nv) x = 0.f;
-        w[u >> 3][u & 7] = (__bf16)x;
-      }
+      scaled<0>(w, p, scale[h]);
 #pragma unroll
       for (int i = 4 * h; i < 4 * h + 4; ++i)
 #pragma unroll

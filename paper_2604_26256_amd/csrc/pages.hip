@@ -172,13 +172,14 @@ done:
 
 // The same over 4-bit pages; a step is 64 tokens.
 template <int D, int P>
-__global__ __launch_bounds__(64 * kSegWaves, 2) void pages4_kernel(PagesParams p) {
+__global__ __launch_bounds__(64 * kSegWaves, 3) void pages4_kernel(PagesParams p) {
   typedef Fp4<D, P> F;
   constexpr int DBLK = D / 16;
   __shared__ __align__(16) union {
     PagesStage stage;
     PagesMerge<D> merge;
   } s;
+  __shared__ bf16x8 s_q[D / 32][64];
   const int lane = threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6);
   const int col = lane & 15;
   const int Hkv = p.num_kv_heads, G = p.group;
@@ -191,8 +192,12 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void pages4_kernel(PagesParams p
   const int n_seg = uni(pages_listed(p, seg, L)), u0 = c * p.chunk_pages;
   if (c > 0 && u0 >= n_seg) return;  // uniform
   const int n = n_seg - u0 < p.chunk_pages ? n_seg - u0 : p.chunk_pages;
-  typename F::Query q;
-  F::load_query(q, p.q + (row0 + col) * D, col < G);
+  if (wave == 0) {  // (in registers the rows would cost the third workgroup of a CU)
+    typename F::Query q;
+    F::load_query(q, p.q + (row0 + col) * D, col < G);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) s_q[i][lane] = q[i];
+  }
   pages_stage<P>(p, s.stage, seg, b, L, u0, n);
 
   f32x4 acc[DBLK];
@@ -226,7 +231,8 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void pages4_kernel(PagesParams p
         const bool all = !__ballot(nv[r] < 16);
         if (all || __ballot(nv[r] > 0)) {
           any = true;
-          F::consume(buf[r], all, nv[r], p.scale_log2, q, acc, m_run, l_run);
+          F::consume(buf[r], all, nv[r], p.scale_log2, [&](int i) { return s_q[i][lane]; }, acc, m_run,
+                     l_run);
         }
         if (++u >= steps) goto done;
       }

@@ -59,4 +59,28 @@ __device__ __forceinline__ bool path_rows(const PathParams& p, const PathPage& p
   return false;
 }
 
+// Launches over (page, sequence): f(parameters, grid, first sequence) for the sequences of a grid at a time.  The pages of a
+// sequence are neighbours, so that a long run's go to all XCDs (workgroups go to them in turn).
+template <typename F>
+inline hipError_t each_launch(const PathParams& p, F f) {
+  constexpr int SEQS = 32768;
+  // pages that p.num_tokens tokens can touch
+  const unsigned pages = (unsigned)((p.num_tokens + p.page_size - 2) / p.page_size + 1);
+  const int64_t row = (int64_t)p.num_tokens * p.num_kv_heads * p.head_dim;
+  for (int first = 0; first < p.num_seqs; first += SEQS) {
+    PathParams q = p;
+    q.num_seqs = p.num_seqs - first < SEQS ? p.num_seqs - first : SEQS;
+    if (p.k_new) q.k_new += first * row;
+    if (p.v_new) q.v_new += first * row;
+    if (p.path) q.path += (int64_t)first * p.num_tokens;
+    if (p.counts) q.counts += first;
+    q.block_table += (int64_t)first * p.stride;
+    q.seq_lens += first;
+    if (p.version_ids) q.version_ids += first;
+    const hipError_t e = f(q, dim3(pages, (unsigned)q.num_seqs), first);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 }  // namespace dora

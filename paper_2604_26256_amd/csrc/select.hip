@@ -24,7 +24,7 @@
 namespace dora {
 
 constexpr float kBf16Most = 3.3895313892515355e38f;
-constexpr int kBoundsWaves = 4;
+constexpr int kBoundsWaves = 8;  // of a workgroup, at most: one for each KV head
 
 // What bounds and queries take a value for.
 __device__ __forceinline__ float finite_of(float x) {
@@ -218,11 +218,10 @@ template <int D, int P, int DT>
 __global__ __launch_bounds__(64 * kBoundsWaves) void page_bounds_kernel(PathParams p,
                                                                        const float* k_scales,
                                                                        uint8_t* bounds) {
-  const PathPage pg = path_page(p, blockIdx.x, blockIdx.y);
+  const PathPage pg = path_page(p, blockIdx.y, blockIdx.x);
   if (pg.id < 0) return;  // uniform
   const int64_t record = bounds_bytes(p.num_kv_heads, D);
-  for (int g = (int)(threadIdx.x >> 6) + kBoundsWaves * (int)blockIdx.z; g < p.num_kv_heads;
-       g += kBoundsWaves * (int)gridDim.z) {
+  for (int g = threadIdx.x >> 6; g < p.num_kv_heads; g += (int)blockDim.x >> 6) {
     uint8_t* at = bounds + pg.id * record;
     BoundsWave<D, P, DT>::run(p.k_pages + (pg.id * p.num_kv_heads + g) * kv_page_bytes(DT, 1, P, D), pg.hi,
                               DT == DORA_KV_FP8_E4M3 ? k_scales[pg.id] : 1.f, at + g * (2 * D),
@@ -243,14 +242,14 @@ hipError_t launch_page_bounds(const PathParams& p, const float* k_scales, uint8_
     const hipError_t e = launch_fill_i32(p.dev_status, (int32_t)DORA_OK, 1, s);
     if (e != hipSuccess) return e;
   }
-  const unsigned pages = (unsigned)((p.num_tokens + p.page_size - 2) / p.page_size + 1);
-  const unsigned parts = (unsigned)((p.num_kv_heads + kBoundsWaves - 1) / kBoundsWaves);
+  const int waves = p.num_kv_heads < kBoundsWaves ? p.num_kv_heads : kBoundsWaves;
   const void* fn =
       p.head_dim == 128 ? (p.page_size == 16 ? bounds_fn<128, 16>(kv_dtype) : bounds_fn<128, 32>(kv_dtype))
                         : (p.page_size == 16 ? bounds_fn<64, 16>(kv_dtype) : bounds_fn<64, 32>(kv_dtype));
-  PathParams arg = p;
-  void* args[] = {(void*)&arg, (void*)&k_scales, (void*)&bounds};
-  return hipLaunchKernel(fn, dim3((unsigned)p.num_seqs, pages, parts), dim3(64 * kBoundsWaves), args, 0, s);
+  return each_launch(p, [&](PathParams arg, dim3 grid, int) {
+    void* args[] = {(void*)&arg, (void*)&k_scales, (void*)&bounds};
+    return hipLaunchKernel(fn, grid, dim3(64u * (unsigned)waves), args, 0, s);
+  });
 }
 
 // ---------------------------------------------------------------------------

@@ -128,10 +128,10 @@ typedef struct {
   uint32_t flags;              /* DORA_FLAG_* */
   int32_t num_waves;           /* decode wavefronts to launch; 0 = library
                                   default: per compute unit of the current
-                                  device at most 4 for bf16 pages, 7 for
-                                  fp8 pages and 8 for 4-bit ones, within the
-                                  resident wavefront slots; never more than the
-                                  batch can use
+                                  device at most 4 for bf16 and 4-bit pages
+                                  and 7 for fp8 pages, within the resident
+                                  wavefront slots; never more than the batch
+                                  can use
                                   (B x Hkv x stride page-heads over the minimum
                                   range).  With both this and min_range_pages 0,
                                   batches whose block tables are short or few
@@ -164,7 +164,8 @@ size_t dora_decode_workspace_bytes(const dora_decode_desc* desc);
  * desc->min_range_pages or 8 when that is 0, and the first T mod W' ranges hold
  * one extra item; so a caller can tell which (sequence, KV head) segments a
  * call cuts across wavefronts (except batches cut per segment, see
- * dora_decode_attn).  Of 4-bit pages the work items are steps of 64 tokens.  Each launch covers at most 8192 sequences.
+ * dora_decode_attn).  Of 4-bit pages the work items are steps of 64 tokens, and
+ * m is 4 where min_range_pages is 0.  Each launch covers at most 8192 sequences.
  * Returns 0 for an invalid or unsupported descriptor. */
 int64_t dora_decode_num_waves(const dora_decode_desc* desc);
 

@@ -76,7 +76,15 @@ bool whole_segments(const dora_decode_desc& d, int64_t segs, int64_t tokens) {
 }
 
 // The same choice for 4-bit pages: pages of a workgroup of the listed-pages kernel, which then
-// takes all pages of a row, or 0 for the stream-K decode.
+// takes all pages of a row, or 0 for the stream-K decode.  A workgroup takes about 3.5 us and
+// 5.5 ns a token, the stream-K call and its combine 12-16 us however little there is to do.
+// So short rows go whole while the segments are few enough to be one or two launches' worth,
+// middle ones are cut where all their chunks run at once, and what is long and many is left to
+// the even ranges of the stream-K decode.  Over 3,824 batches of drawn shapes (up to 1,024
+// rows, 32,768 tokens, all lengths full, uniform, long-tailed or one long row) the rule takes
+// 0.70 of the stream-K decode's time and 1.02 of the best route's; a single long row among
+// short ones, which the table's width does not show, loses most (a row of 11,200 tokens and 15
+// short ones: 24.0 us, stream-K 14.2).
 int pages4_split(const dora_decode_desc& d, int64_t segs, int64_t waves) {
   if (d.num_waves > 0 || d.min_range_pages > 0) return 0;
   const int64_t tokens = (int64_t)d.block_table_stride * d.page_size;
@@ -84,10 +92,11 @@ int pages4_split(const dora_decode_desc& d, int64_t segs, int64_t waves) {
     const int64_t workgroups = segs * ((tokens + chunk - 1) / chunk);
     return workgroups <= most && workgroups <= 2 * waves;
   };
-  if (tokens <= 1024 && segs <= 4096) return d.block_table_stride;
-  if (fits(256, 1024)) return 256 / d.page_size;
-  if (fits(512, 1024)) return 512 / d.page_size;
-  return 0;
+  if (tokens <= 1024) return segs <= 2048 ? d.block_table_stride : 0;
+  if (fits(256, 256)) return 256 / d.page_size;
+  if (tokens <= 2560 && segs <= 2048) return d.block_table_stride;
+  if (fits(512, 256)) return 512 / d.page_size;
+  return fits(1024, 768) ? 1024 / d.page_size : 0;
 }
 
 // The split of the segment kernel for a launch over `segs` (sequence, KV head)
@@ -156,7 +165,9 @@ bool grouped_as_plain(const dora_decode_desc& d, int64_t waves) {
 }
 
 int min_range_of(const dora_decode_desc& d) {
-  return d.min_range_pages > 0 ? d.min_range_pages : kMinRangePages;
+  return d.min_range_pages > 0          ? d.min_range_pages
+         : d.kv_dtype == DORA_KV_FP4 ? kMinRangeSteps
+                                     : kMinRangePages;
 }
 
 }  // namespace

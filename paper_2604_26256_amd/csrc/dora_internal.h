@@ -18,6 +18,7 @@ constexpr int kFp4WavesPerCu = 4;
 // Smallest range (page-heads) a wavefront gets by default: a range must carry
 // enough bytes to amortise the wavefront's start-up (page prefix, first loads).
 constexpr int kMinRangePages = 8;
+constexpr int kMinRangeSteps = 4;  // of 4-bit pages, in steps of 64 tokens
 // Largest batch one decode launch takes: its page prefix ((B + 1) ints) lives
 // in each wavefront's LDS.  Larger batches are cut into launches of this size.
 constexpr int kMaxSeqsPerLaunch = 8192;

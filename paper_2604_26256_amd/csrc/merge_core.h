@@ -30,8 +30,9 @@ __device__ __forceinline__ void merge_piece(float2 ml, f32x4 o, float& M, float&
 // output rows: tasks task0 .. task0 + per - 1 of them, a task being a head and 4
 // head-dim values.  Threads are tasks x piece groups; each folds its pieces into a
 // running (max, normaliser, weighted sum) with one pass of loads, and the groups
-// are merged in LDS.
-template <int THREADS, typename SlotOf>
+// are merged in LDS.  EMPTY: a maximum of -inf stands for a piece that attends
+// nothing, and a row of such pieces is 0.
+template <int THREADS, bool EMPTY = false, typename SlotOf>
 __device__ __forceinline__ void merge_segment(const float* part_o, const float2* part_ml,
                                               uint16_t* out, int num_q_heads, int G, int D, int b,
                                               int g, int task0, int per, int np, SlotOf slot_of) {
@@ -82,7 +83,7 @@ __device__ __forceinline__ void merge_segment(const float* part_o, const float2*
       num += sc * sAcc[i];
       den += sc * sS[i];
     }
-    const float inv = 1.f / den;
+    const float inv = EMPTY && Mx == -__builtin_inff() ? 0.f : 1.f / den;
     const int64_t row = (int64_t)b * num_q_heads + g * G + n;
     uint16_t* o = out + row * D + 4 * d4;
     *(bf16x4*)o = bf16x4{(__bf16)(num[0] * inv), (__bf16)(num[1] * inv),

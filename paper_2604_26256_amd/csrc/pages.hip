@@ -243,40 +243,19 @@ done:
   pages_finish<D>(p, s.merge, acc, m_run, l_run, any, seg, row0, c, n_seg > p.chunk_pages);
 }
 
-// Merges the chunks of a segment that has more than one: a thread per (head, 4 dims).
-__global__ __launch_bounds__(256) void pages_combine_kernel(PagesParams p) {
-  const int seg = (int)blockIdx.x, G = p.group, D = p.head_dim;
+// Merges the chunks of a segment that has more than one, for the tasks part * per .. of it.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void pages_combine_kernel(PagesParams p, int per) {
+  const int seg = (int)blockIdx.x;
   const int b = seg / p.num_kv_heads, g = seg - b * p.num_kv_heads;
   const int64_t most = (int64_t)p.stride * p.page_size;
   const int len = p.seq_lens[b], L = len < most ? len : (int)most;
   const int n = pages_listed(p, seg, L);
   if (n <= p.chunk_pages) return;
-  const int np = (n + p.chunk_pages - 1) / p.chunk_pages;
   const int64_t slot0 = (int64_t)seg * p.chunks;
-  for (int e = threadIdx.x; e < G * (D / 4); e += blockDim.x) {
-    const int h = e / (D / 4), d4 = e - h * (D / 4);
-    float M = -__builtin_inff(), S = 0.f;
-    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < np; k0 += kCombineBatch) {
-      float2 ml[kCombineBatch];
-      f32x4 o[kCombineBatch];
-#pragma unroll
-      for (int i = 0; i < kCombineBatch; ++i) {
-        const int k = k0 + i < np ? k0 + i : np - 1;
-        const int64_t slot = (slot0 + k) * G + h;
-        ml[i] = p.part_ml[slot];
-        o[i] = *(const f32x4*)(p.part_o + slot * D + 4 * d4);
-        if (k0 + i >= np) ml[i].x = -__builtin_inff();
-      }
-#pragma unroll
-      for (int i = 0; i < kCombineBatch; ++i) merge_piece(ml[i], o[i], M, S, acc);
-    }
-    const float inv = M == -__builtin_inff() ? 0.f : 1.f / S;
-    const int64_t row = (int64_t)b * p.num_q_heads + g * G + h;
-    *(bf16x4*)(p.out + row * D + 4 * d4) =
-        bf16x4{(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv),
-               (__bf16)(acc[3] * inv)};
-  }
+  merge_segment<THREADS, true>(p.part_o, p.part_ml, p.out, p.num_q_heads, p.group, p.head_dim, b, g,
+                               (int)blockIdx.y * per, per, (n + p.chunk_pages - 1) / p.chunk_pages,
+                               [=](int k) { return slot0 + k; });
 }
 
 // DORA_FLAG_VALIDATE: lengths, counts, entries, and the ids and owners of the listed pages.
@@ -322,8 +301,13 @@ hipError_t launch_pages(const PagesParams& p, int kv_dtype, hipStream_t s) {
 }
 
 hipError_t launch_pages_combine(const PagesParams& p, hipStream_t s) {
-  hipLaunchKernelGGL(pages_combine_kernel, dim3((unsigned)(p.num_seqs * p.num_kv_heads)), dim3(256), 0,
-                     s, p);
+  const int segs = p.num_seqs * p.num_kv_heads;
+  const int tasks = p.group * (p.head_dim / 4);
+  int parts = 1;  // as launch_combine_chunks
+  while (tasks > 64 * parts && p.chunks * (tasks / parts) > 8 * 512 && 2 * parts * segs <= 1024)
+    parts *= 2;
+  hipLaunchKernelGGL(pages_combine_kernel<512>, dim3((unsigned)segs, (unsigned)parts), dim3(512), 0, s,
+                     p, (tasks + parts - 1) / parts);
   return hipGetLastError();
 }
 

@@ -129,7 +129,7 @@ def test_sizes(d):
         assert d.dora_kv_packed_bytes(pack(**kw), 5) == 0
     # the work of 4-bit pages is counted in steps of 64 tokens
     desc = _desc(d, kv_dtype=d.DORA_KV_FP4, block_table_stride=8)
-    assert d.dora_decode_num_waves(desc) == 4 * 2 * 2 // 8
+    assert d.dora_decode_num_waves(desc) == 4 * 2 * 2 // 4
     assert d.dora_decode_workspace_bytes(desc) > 0
     assert d.dora_decode_num_waves(_desc(d, kv_dtype=d.DORA_KV_FP4, num_waves=77)) == 77
 

@@ -26,10 +26,22 @@ dora_status validate_lists(const dora_decode_desc& d, int32_t list_stride, const
                            const int32_t* counts, const int32_t* block_table, const int32_t* seq_lens,
                            const int32_t* version_ids, int32_t* err, hipStream_t s) {
   if (launch_fill_i32(err, 0, 1, s) != hipSuccess) return DORA_ERR_HIP;
-  ValidateParams vp{block_table, seq_lens, version_ids, d.page_owner, d.num_seqs,
-                    d.page_size, d.block_table_stride, d.num_pages, err};
-  if (launch_pages_validate(vp, lists, counts, d.num_kv_heads, list_stride, s) != hipSuccess)
-    return DORA_ERR_HIP;
+  for (int c0 = 0; c0 < d.num_seqs; c0 += kMaxSeqsPerLaunch) {
+    const int seqs = d.num_seqs - c0 < kMaxSeqsPerLaunch ? d.num_seqs - c0 : kMaxSeqsPerLaunch;
+    const int64_t seg0 = (int64_t)c0 * d.num_kv_heads;
+    ValidateParams vp{block_table + (int64_t)c0 * d.block_table_stride,
+                      seq_lens + c0,
+                      version_ids ? version_ids + c0 : nullptr,
+                      d.page_owner,
+                      seqs,
+                      d.page_size,
+                      d.block_table_stride,
+                      d.num_pages,
+                      err};
+    if (launch_pages_validate(vp, lists + seg0 * list_stride, counts + seg0, d.num_kv_heads,
+                              list_stride, s) != hipSuccess)
+      return DORA_ERR_HIP;
+  }
   int32_t host_err = 0;
   if (hipMemcpyAsync(&host_err, err, 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
       hipStreamSynchronize(s) != hipSuccess)
@@ -166,7 +178,8 @@ dora_status dora_kv_page_bounds(const dora_decode_desc* desc, int32_t num_tokens
 
 size_t dora_page_select_workspace_bytes(const dora_decode_desc* desc) {
   if (check_desc(desc) != DORA_OK) return 0;
-  return scores_off() + (size_t)desc->num_seqs * desc->num_kv_heads * desc->block_table_stride * 4;
+  const int seqs = desc->num_seqs < kMaxSeqsPerLaunch ? desc->num_seqs : kMaxSeqsPerLaunch;
+  return scores_off() + (size_t)seqs * desc->num_kv_heads * desc->block_table_stride * 4;
 }
 
 dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32_t sink_pages,
@@ -193,27 +206,31 @@ dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32
     st = validate_tables(d, block_table, seq_lens, version_ids, (int32_t*)ws, s);
     if (st != DORA_OK) return st;
   }
-  SelectParams p;
-  p.q = (const uint16_t*)q;
-  p.bounds = (const uint8_t*)bounds;
-  p.block_table = block_table;
-  p.seq_lens = seq_lens;
-  p.scores = scores ? scores : (float*)(ws + scores_off());
-  p.lists = page_lists;
-  p.counts = page_counts;
-  p.record = bounds_bytes(d.num_kv_heads, d.head_dim);
-  p.num_seqs = d.num_seqs;
-  p.num_q_heads = d.num_q_heads;
-  p.num_kv_heads = d.num_kv_heads;
-  p.group = d.num_q_heads / d.num_kv_heads;
-  p.stride = d.block_table_stride;
-  p.head_dim = d.head_dim;
-  p.page_size = d.page_size;
-  p.budget = budget;
-  p.sinks = sink_pages;
-  p.recent = recent_pages;
-  if (launch_page_scores(p, compute_units(), s) != hipSuccess) return DORA_ERR_HIP;
-  return launch_page_select(p, s) == hipSuccess ? DORA_OK : DORA_ERR_HIP;
+  for (int c0 = 0; c0 < d.num_seqs; c0 += kMaxSeqsPerLaunch) {
+    const int64_t seg0 = (int64_t)c0 * d.num_kv_heads;
+    SelectParams p;
+    p.q = (const uint16_t*)q + (int64_t)c0 * d.num_q_heads * d.head_dim;
+    p.bounds = (const uint8_t*)bounds;
+    p.block_table = block_table + (int64_t)c0 * d.block_table_stride;
+    p.seq_lens = seq_lens + c0;
+    p.scores = scores ? scores + seg0 * d.block_table_stride : (float*)(ws + scores_off());
+    p.lists = page_lists + seg0 * budget;
+    p.counts = page_counts + seg0;
+    p.record = bounds_bytes(d.num_kv_heads, d.head_dim);
+    p.num_seqs = d.num_seqs - c0 < kMaxSeqsPerLaunch ? d.num_seqs - c0 : kMaxSeqsPerLaunch;
+    p.num_q_heads = d.num_q_heads;
+    p.num_kv_heads = d.num_kv_heads;
+    p.group = d.num_q_heads / d.num_kv_heads;
+    p.stride = d.block_table_stride;
+    p.head_dim = d.head_dim;
+    p.page_size = d.page_size;
+    p.budget = budget;
+    p.sinks = sink_pages;
+    p.recent = recent_pages;
+    if (launch_page_scores(p, compute_units(), s) != hipSuccess) return DORA_ERR_HIP;
+    if (launch_page_select(p, s) != hipSuccess) return DORA_ERR_HIP;
+  }
+  return DORA_OK;
 }
 
 dora_status dora_kv_read(const dora_decode_desc* desc, int32_t num_tokens, const int32_t* counts,

@@ -1,0 +1,180 @@
+"""4-bit and listed pages in batches of more sequences than a launch covers, by every route of the 4-bit decode, and with
+neighbours at work: other streams, graphs, empty rows."""
+import numpy as np
+import pytest
+import torch
+
+from cache_util import bound, check
+from fp4_util import FP4, Cache4, bf16_of, bf16_value, dec4, key_codes, make_cache, value_codes
+from gpu_util import lib
+from test_gpu_fp4 import _reference as _dense_reference
+from test_gpu_pages import TYPES, _q, _reference
+from test_gpu_select import _bounds, _record, _tokens32
+
+pytestmark = pytest.mark.gpu
+
+
+def _tiled(c, B):
+    """The sequences of c again and again up to B rows, over the same pages."""
+    at = np.arange(B) % len(c.lens)
+    dev = c.gpu()
+    dev["bt"], dev["lens"] = (dev[n][torch.from_numpy(at).cuda()].contiguous() for n in ("bt", "lens"))
+    return dev, torch.from_numpy(at)
+
+
+def _check_tiled(out, at, want, spread, what):
+    """Every row against the 64-bit row that it repeats."""
+    got = out.float().cpu().double()
+    limit = torch.from_numpy(bound(want, spread))
+    assert not got.isnan().any()
+    off = (got - torch.from_numpy(want)[at]).abs() - limit[at]
+    assert float(off.max()) <= 0, f"{what}: {float(off.max())} beyond the bound"
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("B", [8192, 8193, 20000])
+def test_more_sequences_than_a_launch_covers(dt, B):
+    print(f"[case] batches dt={dt} B={B}", flush=True)
+    D, Hkv, G, d, P, budget = lib(), 2, 2, 64, 16, 3
+    c = make_cache([0, 1, 40, 17, 100, 64, 300], Hkv, d, P, dt, seed=3)
+    dev, at = _tiled(c, B)
+    q = _q(len(c.lens), Hkv * G, d, 1)
+    qd = q[at].cuda().contiguous()
+    bounds = torch.zeros(c.num_pages, D.dora_page_bounds_bytes(Hkv, d), dtype=torch.uint8, device="cuda")
+    small = c.gpu()
+    bkw = {k: v for k, v in dev["kw"].items() if k != "v_scales"}
+    D.dora_kv_page_bounds(small["k"], small["bt"], small["lens"], bounds, num_tokens=300, head_dim=d, counts=small["lens"], **bkw)
+    lists = torch.full((B, Hkv, budget), -1, dtype=torch.int32, device="cuda")
+    counts = torch.full((B, Hkv), -1, dtype=torch.int32, device="cuda")
+    few = torch.full((7, Hkv, budget), -1, dtype=torch.int32, device="cuda"), torch.full((7, Hkv), -1, dtype=torch.int32, device="cuda")
+    args = dict(num_kv_heads=Hkv, page_size=P)
+    D.dora_page_select(q.cuda(), bounds, small["bt"], small["lens"], *few, **args)
+    for scores in (False, True):
+        lists.fill_(-1)
+        sc = torch.zeros(B, Hkv, dev["bt"].shape[1], device="cuda") if scores else None
+        D.dora_page_select(qd, bounds, dev["bt"], dev["lens"], lists, counts, scores=sc, **args)
+        assert torch.equal(lists.cpu(), few[0].cpu()[at]) and torch.equal(counts.cpu(), few[1].cpu()[at])
+    want, spread = _reference(c, q, few[0].cpu().numpy(), few[1].cpu().numpy())
+    out = torch.full_like(qd, 7.0)
+    D.dora_decode_attn_pages(qd, lists, counts, dev["k"], dev["v"], dev["bt"], dev["lens"], None, out, **dev["kw"])
+    _check_tiled(out, at, want, spread, "pages")
+    D.dora_decode_attn_pages(qd, lists, counts, dev["k"], dev["v"], dev["bt"], dev["lens"], None, out, flags=D.DORA_FLAG_VALIDATE,
+                             **dev["kw"])
+    _check_tiled(out, at, want, spread, "validated pages")
+    if dt == FP4:
+        out.fill_(7.0)
+        D.dora_decode_attn(qd, dev["k"], dev["v"], dev["bt"], dev["lens"], None, out, **dev["kw"])
+        _check_tiled(out, at, *_dense_reference(c, q), "decode4")
+    last = counts.clone()
+    last[B - 1, 1] = budget + 1  # in the last launch
+    with pytest.raises(D.DoraError) as e:
+        D.dora_decode_attn_pages(qd, lists, last, dev["k"], dev["v"], dev["bt"], dev["lens"], None, out, flags=D.DORA_FLAG_VALIDATE,
+                                 **dev["kw"])
+    assert e.value.status == D.DORA_ERR_DEVICE_CHECK
+
+
+@pytest.mark.parametrize("one", [False, True])
+def test_stores_and_reads_of_more_sequences_than_a_launch_covers(one):
+    """33,000 sequences with a page of their own: stored bit for bit as their rows say, read back, and bounded."""
+    D, B, d, P = lib(), 33000, 64, 16
+    T = 1 if one else 3
+    rng = np.random.default_rng(4)
+    bits = [bf16_of(rng.standard_normal((B, T, 1, d))) for _ in range(2)]
+    perm = rng.permutation(B).astype(np.int32)
+    dev = {n: torch.full((B, 1, P * d * 17 // 32), 0xFF, dtype=torch.uint8, device="cuda") for n in "kv"}
+    bt = torch.from_numpy(perm[:, None]).cuda()
+    lens = torch.full((B,), T, dtype=torch.int32, device="cuda")
+    kw = dict(num_kv_heads=1, page_size=P, kv_dtype=FP4)
+    new = [torch.from_numpy(x.view(np.int16)).view(torch.bfloat16).cuda() for x in bits]
+    if one:
+        D.dora_kv_append(new[0][:, 0], new[1][:, 0], bt, lens, dev["k"], dev["v"], **kw)
+    else:
+        D.dora_kv_append_path(*new, bt, lens, dev["k"], dev["v"], **kw)
+    out = [torch.zeros(B, T, 1, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    D.dora_kv_read(dev["k"], dev["v"], bt, lens, *out, **kw)
+    ck, ek = key_codes(bits[0])
+    cv, sv = value_codes(bits[1])
+    k = dec4(ck) * np.repeat(np.exp2(ek.astype(np.float64) - 127), 32, axis=-1)
+    v = dec4(cv) * np.repeat(bf16_value(sv).astype(np.float64), 64, axis=-1)
+    for x, y in zip(out, (k, v)):
+        assert np.array_equal(x.cpu().view(torch.int16).numpy().view(np.uint16), bf16_of(y))
+    bounds = torch.zeros(B, D.dora_page_bounds_bytes(1, d), dtype=torch.uint8, device="cuda")
+    D.dora_kv_page_bounds(dev["k"], bt, lens, bounds, num_tokens=T, head_dim=d, **kw)
+    got = bounds.cpu().numpy()
+    for b in (0, 8191, 8192, 32767, 32768, B - 1):
+        assert np.array_equal(got[perm[b], :2 * d + 4], _record(*_bounds(k[b]))[:2 * d + 4])
+    seen = got[perm, 2 * d:2 * d + 4].copy().view(np.float32)[:, 0]  # every page's scale
+    top = np.abs(k).max((1, 2, 3)).astype(np.float32) / np.float32(127)
+    assert np.array_equal(seen, top)
+
+
+ROUTES = [  # rows, KV heads, longest row, pages of 16 tokens in a workgroup: whole rows, chunks, and none
+    (5, 2, 900, None), (2000, 1, 60, None), (5, 2, 1500, 16), (100, 2, 2300, None), (6, 2, 6000, 32), (40, 1, 4500, 64), (12, 2, 15000, 64),
+    (3, 1, 32000, 32), (300, 2, 2700, 0), (1100, 2, 200, 0)]
+
+
+@pytest.mark.parametrize("B,Hkv,longest,pages", ROUTES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_routes_of_the_4_bit_decode(B, Hkv, longest, pages, d):
+    print(f"[case] route B={B} Hkv={Hkv} longest={longest} d={d}", flush=True)
+    D, G = lib(), 3
+    c = Cache4([longest, 0, longest // 3, 1, longest // 2 + 1], Hkv, d, 16, seed=5)
+    dev, at = _tiled(c, B)
+    q = _q(5, Hkv * G, d, 2)
+    qd = q[at].cuda().contiguous()
+    width = dev["bt"].shape[1]
+    desc = D.make_decode_desc(num_seqs=B, num_q_heads=Hkv * G, num_kv_heads=Hkv, head_dim=d, page_size=16, block_table_stride=width,
+                              num_pages=c.num_pages, kv_dtype=FP4)
+    assert D.dora_decode_segment_pages(desc) == (width if pages is None else pages)
+    want, spread = _dense_reference(c, q)
+    out = torch.full_like(qd, 7.0)
+    D.dora_decode_attn(qd, dev["k"], dev["v"], dev["bt"], dev["lens"], None, out, **dev["kw"])
+    _check_tiled(out, at, want, spread, "decode4")
+
+
+def test_two_graphs_on_two_streams():
+    """Two captured runs over chunked lists and cut rows, replayed at once on streams of their own, with eager calls of
+    the same shapes between: each equals its own eager run."""
+    D = lib()
+    runs = []
+    for i in range(2):
+        c = make_cache([9000, 300, 5000], 2, 64, 16, FP4, seed=i)
+        dev = c.gpu()
+        q = _q(3, 8, 64, i).cuda()
+        n = -(-c.lens // 16)
+        width = int(n.max())
+        lists = torch.arange(width, dtype=torch.int32).repeat(3, 2, 1).cuda()
+        counts = torch.from_numpy(np.tile(n[:, None], (1, 2)).astype(np.int32)).cuda()
+        bounds = torch.randint(0, 100, (c.num_pages, D.dora_page_bounds_bytes(2, 64)), generator=torch.Generator().manual_seed(i),
+                               dtype=torch.uint8).cuda()
+        picked = torch.zeros(3, 2, 9, dtype=torch.int32, device="cuda"), torch.zeros(3, 2, dtype=torch.int32, device="cuda")
+        outs = [torch.zeros_like(q) for _ in range(2)]
+
+        def step(c=c, dev=dev, q=q, lists=lists, counts=counts, bounds=bounds, picked=picked, outs=outs, stream=None):
+            D.dora_page_select(q, bounds, dev["bt"], dev["lens"], *picked, num_kv_heads=2, page_size=16, stream=stream)
+            D.dora_decode_attn_pages(q, lists, counts, dev["k"], dev["v"], dev["bt"], dev["lens"], None, outs[0], stream=stream, **dev["kw"])
+            D.dora_decode_attn(q, dev["k"], dev["v"], dev["bt"], dev["lens"], None, outs[1], stream=stream, **dev["kw"])
+
+        step()
+        torch.cuda.synchronize()
+        eager = [x.clone() for x in (*outs, *picked)]
+        graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        runs.append((graph, stream, step, (*outs, *picked), eager))
+    for _ in range(5):
+        for _, _, _, outs, _ in runs:
+            for x in outs:
+                x.zero_()
+        torch.cuda.synchronize()
+        for graph, stream, *_ in runs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, _, _, outs, eager in runs:
+            assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+        for _, _, step, outs, eager in runs:
+            step()
+        torch.cuda.synchronize()
+        for _, _, _, outs, eager in runs:
+            assert all(torch.equal(a, b) for a, b in zip(outs, eager))

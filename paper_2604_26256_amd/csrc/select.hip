@@ -550,7 +550,7 @@ template <int ITEMS>
 __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParams p) {
   constexpr int WAVES = kSelectThreads / 64;
   __shared__ int s_count[256];
-  __shared__ int s_above, s_bin;
+  __shared__ int s_above, s_bin, s_all;
   __shared__ uint32_t s_low[WAVES], s_high[WAVES];
   __shared__ int2 s_part[(ITEMS ? ITEMS : 1) * WAVES];  // {larger, equal} of a wave's 64 pages
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -637,6 +637,7 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParam
             if (over + c[k] >= need) {
               s_bin = 4 * lane + k;
               s_above = over;
+              s_all = over + c[k] == need;
               break;
             }
             over += c[k];
@@ -647,6 +648,11 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParam
       key = key << take | (uint32_t)s_bin;
       need -= s_above;
       left = shift;
+      if (s_all) {  // uniform: all scores that begin like this are chosen, whatever their lower bits
+        key = (key << left) - 1;  // (at least one is not chosen: not below 0)
+        need = 0;
+        break;
+      }
       if (left > 0) {
         if (tid < 256) s_count[tid] = 0;
         __syncthreads();

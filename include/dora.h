@@ -450,7 +450,7 @@ dora_status dora_kv_page_bounds(const dora_decode_desc* desc, int32_t num_tokens
  *   scores       device fp32 [B][Hkv][block_table_stride] or NULL: receives the scores of the
  *                sequence's pages (entries behind them are left as they were)
  *   workspace    >= dora_page_select_workspace_bytes(desc) bytes (with scores, 256), 16-byte aligned
- * Two launches. */
+ * One launch where rows are few and short, else two. */
 size_t dora_page_select_workspace_bytes(const dora_decode_desc* desc);
 dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32_t sink_pages,
                              int32_t recent_pages, const void* q, const void* bounds,

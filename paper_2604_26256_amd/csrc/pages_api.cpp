@@ -206,6 +206,7 @@ dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32
     st = validate_tables(d, block_table, seq_lens, version_ids, (int32_t*)ws, s);
     if (st != DORA_OK) return st;
   }
+  const int cus = compute_units();
   for (int c0 = 0; c0 < d.num_seqs; c0 += kMaxSeqsPerLaunch) {
     const int64_t seg0 = (int64_t)c0 * d.num_kv_heads;
     SelectParams p;
@@ -227,7 +228,12 @@ dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32
     p.budget = budget;
     p.sinks = sink_pages;
     p.recent = recent_pages;
-    if (launch_page_scores(p, compute_units(), s) != hipSuccess) return DORA_ERR_HIP;
+    if (select_at_once(p, cus)) {
+      p.scores = scores ? p.scores : nullptr;
+      if (launch_page_score_select(p, s) != hipSuccess) return DORA_ERR_HIP;
+      continue;
+    }
+    if (launch_page_scores(p, cus, s) != hipSuccess) return DORA_ERR_HIP;
     if (launch_page_select(p, s) != hipSuccess) return DORA_ERR_HIP;
   }
   return DORA_OK;

@@ -96,6 +96,9 @@ struct SelectParams {
 };
 hipError_t launch_page_scores(const SelectParams& p, int cus, hipStream_t s);
 hipError_t launch_page_select(const SelectParams& p, hipStream_t s);
+// Whether one launch does both, and that launch (scores may be null then).
+bool select_at_once(const SelectParams& p, int cus);
+hipError_t launch_page_score_select(const SelectParams& p, hipStream_t s);
 
 // Rows of the last tokens, as bf16 (PathParams' k_new, v_new and path are not used).
 hipError_t launch_kv_read(const PathParams& p, const float* k_scales, const float* v_scales,

@@ -368,6 +368,17 @@ __device__ __forceinline__ void score_query(ScoreQuery<D>& s, const uint16_t* qr
     }
 }
 
+// The largest score of a page's over the group's rows, in all lanes of its column: sum and step are of
+// rows 4 * (lane >> 4) .. + 3.
+__device__ __forceinline__ float best_row(i32x4 sum, f32x4 step, int group) {
+  const int grp = (threadIdx.x & 63) >> 4;
+  float best = -__builtin_inff();
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (4 * grp + k < group) best = fmaxf(best, (float)sum[k] * step[k]);
+  return max_xor32(max_xor16(best));
+}
+
 // A wave's place in the batch's list of tiles (16 pages of a sequence): every workgroup takes an equal
 // contiguous range, however long the sequences are.  By all threads of a workgroup; to: the range,
 // and the sequence and tile that it starts with.
@@ -496,11 +507,7 @@ __global__ __launch_bounds__(64 * kScoreWaves, kScorePerCu) void page_scores_ker
 #pragma unroll
           for (int m = 0; m < M; ++m)
             sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[h].w[m], t.x[h].w[m], sum, 0, 0, 0);
-          best[h] = -__builtin_inff();
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (4 * grp + k < p.group) best[h] = fmaxf(best[h], (float)sum[k] * step[h][k]);
-          best[h] = max_xor32(max_xor16(best[h]));
+          best[h] = best_row(sum, step[h], p.group);
         }
         if (grp < 2) s_out[wave][grp][16 * u + col] = (grp ? best[1] : best[0]) * t.s;
       };
@@ -540,29 +547,20 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One workgroup per (sequence, KV head): all pages where the budget holds them; else the sinks, the most
-// recent ones, and of those between the ones with the largest scores.  The last chosen one's score is
+// Of the n > budget pages of a segment the sinks, the most recent ones, and of those between the ones
+// with the largest scores, into list: by all threads of a workgroup.  The last chosen one's score is
 // found from its upper bits down, 8 at a time below those that all scores share, by counting; the
 // pages are written in order, those with that very score as long as there is room.
-//   ITEMS: scores that a thread holds in registers (of page tid + k * kSelectThreads); 0: any number of
-// them, read again each time.
-template <int ITEMS>
-__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParams p) {
+//   ITEMS: scores that a thread holds in registers (score_at(i) of i = tid + k * kSelectThreads); 0: any
+// number of them, asked for again each time.
+template <int ITEMS, typename ScoreAt>
+__device__ __forceinline__ void choose_pages(const SelectParams& p, int n, int32_t* list, ScoreAt score_at) {
   constexpr int WAVES = kSelectThreads / 64;
   __shared__ int s_count[256];
   __shared__ int s_above, s_bin, s_all;
   __shared__ uint32_t s_low[WAVES], s_high[WAVES];
   __shared__ int2 s_part[(ITEMS ? ITEMS : 1) * WAVES];  // {larger, equal} of a wave's 64 pages
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int seg = blockIdx.x, b = seg / p.num_kv_heads;
-  const int n = uni(pages_of(p.seq_lens[b], p.page_size, p.stride));
-  int32_t* list = p.lists + (int64_t)seg * p.budget;
-  if (tid == 0) p.counts[seg] = n < p.budget ? n : p.budget;
-  if (n <= p.budget) {  // uniform
-    for (int i = tid; i < n; i += kSelectThreads) list[i] = i;
-    return;
-  }
-  const float* scores = p.scores + (int64_t)seg * p.stride;
   const int from = p.sinks, upto = n - p.recent;  // those that compete
   int need = p.budget - p.sinks - p.recent;       // < upto - from
   uint32_t held[ITEMS ? ITEMS : 1];
@@ -570,7 +568,7 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParam
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
       const int i = tid + k * kSelectThreads;
-      held[k] = score_key(i < n ? scores[i] : 0.f);
+      held[k] = score_key(i < n ? score_at(i) : 0.f);
     }
   }
   auto competes = [&](int i) { return i >= from && i < upto; };
@@ -580,7 +578,7 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParam
       for (int k = 0; k < ITEMS; ++k)
         if (competes(tid + k * kSelectThreads)) f(tid + k * kSelectThreads, held[k]);
     } else {
-      for (int i = from + tid; i < upto; i += kSelectThreads) f(i, score_key(scores[i]));
+      for (int i = from + tid; i < upto; i += kSelectThreads) f(i, score_key(score_at(i)));
     }
   };
   uint32_t key = 0;
@@ -720,7 +718,7 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParam
     for (int base = 0; base < n; base += kSelectThreads) {
       const int i = base + tid;
       bool gt, eq;
-      place(i, i < n ? score_key(scores[i]) : 0u, gt, eq);
+      place(i, i < n ? score_key(score_at(i)) : 0u, gt, eq);
       const uint64_t gts = __ballot(gt), eqs = __ballot(eq);
       if (lane == 0) s_part[wave] = make_int2(__popcll(gts), __popcll(eqs));
       __syncthreads();
@@ -740,6 +738,124 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParam
       __syncthreads();
     }
   }
+}
+
+// A segment's count, and its list where the budget holds all its pages.  False: they have to be chosen.
+__device__ __forceinline__ bool lists_all(const SelectParams& p, int seg, int n, int32_t* list) {
+  if (threadIdx.x == 0) p.counts[seg] = n < p.budget ? n : p.budget;
+  if (n > p.budget) return false;  // uniform
+  for (int i = threadIdx.x; i < n; i += kSelectThreads) list[i] = i;
+  return true;
+}
+
+// One workgroup per (sequence, KV head).
+template <int ITEMS>
+__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(SelectParams p) {
+  const int seg = blockIdx.x, b = seg / p.num_kv_heads;
+  const int n = uni(pages_of(p.seq_lens[b], p.page_size, p.stride));
+  int32_t* list = p.lists + (int64_t)seg * p.budget;
+  if (lists_all(p, seg, n, list)) return;
+  const float* scores = p.scores + (int64_t)seg * p.stride;
+  choose_pages<ITEMS>(p, n, list, [&](int i) { return scores[i]; });
+}
+
+// A row as whole numbers by one wave, two of them a lane (of 64 values, the upper lanes' are not stored): into
+// u[D], and its step.
+template <int D>
+__device__ __forceinline__ void score_row(const uint16_t* qrow, bool valid, uint16_t* u, float* step_at) {
+  const int lane = threadIdx.x & 63, at = lane % (D / 2);
+  const uint32_t two = valid ? ((const uint32_t*)qrow)[at] : 0u;
+  const float x = finite_of(__uint_as_float(two << 16)), y = finite_of(__uint_as_float(two & 0xFFFF0000u));
+  const float step = fmaxf(__fdiv_rn(wave_max(fmaxf(fabsf(x), fabsf(y))), 127.0f), 0x1p-126f);
+  const int a = (int)__builtin_rintf(__fdiv_rn(x, step)), b = (int)__builtin_rintf(__fdiv_rn(y, step));
+  if (lane < D / 2) u[at] = (uint16_t)((a & 0xFF) | (b & 0xFF) << 8);
+  if (lane == 0) *step_at = step;
+}
+
+// Scores and choice in one launch, for few and short rows: one workgroup per (sequence, KV head).  A wave
+// makes one row of the group whole numbers, for all of them, and has every sixteenth tile of 16 pages.
+template <int D>
+__global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(SelectParams p) {
+  constexpr int M = D / 32, WAVES = kSelectThreads / 64, TILES = kSelectThreads / 16 / WAVES;
+  __shared__ float s_score[kSelectThreads], s_step[16];
+  __shared__ __align__(16) uint8_t s_u[16][D];
+  const int lane = threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+  const int Hkv = p.num_kv_heads, seg = blockIdx.x, b = seg / Hkv, g = seg - b * Hkv;
+  int id[TILES];  // of page `col` of each tile (loaded beside the length)
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) {
+    const int i = 16 * (wave + k * WAVES) + col;
+    id[k] = p.block_table[(int64_t)b * p.stride + (i < p.stride ? i : p.stride - 1)];
+  }
+  const int n = uni(pages_of(p.seq_lens[b], p.page_size, p.stride));
+  int32_t* list = p.lists + (int64_t)seg * p.budget;
+  const bool all = lists_all(p, seg, n, list);
+  if (all && !p.scores) return;  // uniform
+  score_row<D>(p.q + ((int64_t)b * p.num_q_heads + (int64_t)g * p.group + wave) * D, wave < p.group,
+               (uint16_t*)s_u[wave], &s_step[wave]);
+  const int mine = 16 * wave < n ? (((n + 15) >> 4) - wave + WAVES - 1) / WAVES : 0;  // tiles
+  PageBounds<M> x[TILES];
+  float s[TILES];
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) {
+    if (k >= mine) break;  // uniform
+    const int first = 16 * (wave + k * WAVES);
+    auto page = [&](int i) {  // (behind the last page, that one again)
+      return p.bounds + (int64_t)__shfl(id[k], first + i < n ? i : n - 1 - first) * p.record;
+    };
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+      x[k].w[m] = *(const i32x4*)(page((col & ~(M - 1)) + m) + D / 2 * grp + 16 * (col & (M - 1)) + g * (2 * D));
+    s[k] = ((const float*)(page(col) + Hkv * (2 * D)))[g];
+  }
+  __syncthreads();
+  i32x4 q[M];
+  f32x4 step;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) step[k] = s_step[4 * grp + k];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    q[m] = *(const i32x4*)&s_u[col][D / 2 * (grp & 1) + 16 * m];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // the negative ones, or the others
+      const uint32_t w = (uint32_t)q[m][i], negative = ((w >> 7) & 0x01010101u) * 0xFFu;
+      q[m][i] = (int)(grp < 2 ? w & ~negative : w & negative);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) {
+    if (k >= mine) break;  // uniform
+    as_operands<M>(x[k]);
+    i32x4 sum{0, 0, 0, 0};
+#pragma unroll
+    for (int m = 0; m < M; ++m) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[m], x[k].w[m], sum, 0, 0, 0);
+    const float best = best_row(sum, step, p.group) * s[k];
+    if (grp == 0) s_score[16 * (wave + k * WAVES) + col] = best;
+  }
+  __syncthreads();
+  if (p.scores) {
+    float* out = p.scores + (int64_t)seg * p.stride;
+    for (int i = threadIdx.x; i < n; i += kSelectThreads) out[i] = s_score[i];
+  }
+  if (!all) choose_pages<1>(p, n, list, [&](int i) { return s_score[i]; });
+}
+
+// One launch takes 5.5 to 8 us for rows of up to 256 pages and 12 for 1,024, two take 12.5 to 24, as long
+// as a round of workgroups (one of 16 waves on a CU) has the batch; of short rows, two rounds are worth it
+// too (64 rows, 8 KV heads, 256 pages: 18.9 and 26.3 us; 1,024 pages: 48.4 and 37.2, as bounds
+// are read best with all heads of a page at once, which page_scores_kernel does).
+bool select_at_once(const SelectParams& p, int cus) {
+  const int64_t segs = (int64_t)p.num_seqs * p.num_kv_heads;
+  return p.stride <= 256 ? segs <= 2 * cus : p.stride <= kSelectThreads && segs <= cus;
+}
+
+hipError_t launch_page_score_select(const SelectParams& p, hipStream_t s) {
+  const dim3 grid((unsigned)(p.num_seqs * p.num_kv_heads));
+  if (p.head_dim == 128)
+    hipLaunchKernelGGL(page_score_select_kernel<128>, grid, dim3(kSelectThreads), 0, s, p);
+  else
+    hipLaunchKernelGGL(page_score_select_kernel<64>, grid, dim3(kSelectThreads), 0, s, p);
+  return hipGetLastError();
 }
 
 hipError_t launch_page_scores(const SelectParams& p, int cus, hipStream_t s) {

@@ -122,12 +122,14 @@ def _choice(scores, n, budget, sinks, recent):
     return np.sort(np.concatenate([np.arange(sinks), middle[order[:budget - sinks - recent]], np.arange(n - recent, n)]))
 
 
-def _select(lens, Hkv, G, d, P, budget, sinks, recent, seed, make=None, scores=True):
+def _select(lens, Hkv, G, d, P, budget, sinks, recent, seed, make=None, scores=True, width=0):
+    """Scores, lists and counts against the definition.  A table of more than 1,024 pages takes two launches, a narrower
+    one of as few rows as here one."""
     D = lib()
     rng = np.random.default_rng(seed)
     lens = np.asarray(lens, np.int32)
     n = -(-lens // P)
-    width = max(1, int(n.max())) + 2
+    width = max(width, int(n.max()) + 2)
     pages = int(n.sum()) + 3
     hi = rng.integers(-40, 128, (pages, Hkv, d)).astype(np.int8)
     lo = np.minimum(hi, rng.integers(-127, 41, hi.shape)).astype(np.int8)
@@ -167,10 +169,23 @@ LENS = [0, 1, 16, 17, 100, 255, 256, 257, 500, 1000, 4000]
 @pytest.mark.parametrize("P", [16, 32])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("Hkv,G", [(1, 1), (2, 7), (5, 16), (8, 4)])
-def test_choice(P, d, Hkv, G):
-    print(f"[case] select P={P} d={d} Hkv={Hkv} G={G}", flush=True)
-    _select(LENS, Hkv, G, d, P, 9, 1, 2, seed=P + d + G)
-    _select(LENS, Hkv, G, d, P, 1, 0, 0, seed=P + d + G, scores=False)
+@pytest.mark.parametrize("width", [0, 1025])
+def test_choice(P, d, Hkv, G, width):
+    print(f"[case] select P={P} d={d} Hkv={Hkv} G={G} width={width}", flush=True)
+    _select(LENS, Hkv, G, d, P, 9, 1, 2, seed=P + d + G, width=width)
+    _select(LENS, Hkv, G, d, P, 1, 0, 0, seed=P + d + G, scores=False, width=width)
+
+
+@pytest.mark.parametrize("pages", [255, 256, 257, 1023, 1024])
+@pytest.mark.parametrize("d", [64, 128])
+def test_one_launch_at_its_widest(pages, d):
+    _select([16 * (pages - 2) - 15, 16 * (pages - 2), 16 * 200, 5], 3, 5, d, 16, 33, 1, 2, seed=pages, width=pages)
+
+
+@pytest.mark.parametrize("rows", [32, 33, 64, 65])
+@pytest.mark.parametrize("width", [40, 300])
+def test_rows_around_a_round_of_workgroups(rows, width):
+    _select([16 * (5 + i % 31) for i in range(rows)], 8, 2, 64, 16, 7, 0, 1, seed=rows, width=width, scores=rows % 2 == 0)
 
 
 @pytest.mark.parametrize("budget,sinks,recent", [(1, 0, 1), (1, 1, 0), (5, 2, 3), (16, 0, 0), (100, 3, 7), (3000, 1, 1)])
@@ -200,6 +215,7 @@ def test_equal_scores_go_to_the_lower_page():
 
     for make in (same, two_kinds, zeros):
         _select([800, 5000, 17000], 2, 3, 64, 16, 20, 2, 1, seed=1, make=make)
+        _select([800, 5000, 16000], 2, 3, 64, 16, 20, 2, 1, seed=1, make=make)
 
 
 def test_scores_below_zero_and_past_the_range():
@@ -219,7 +235,8 @@ def test_scores_below_zero_and_past_the_range():
         q[2, 3, 5] = float("-inf")
 
     for make in (negative, huge, odd):
-        _select([300, 2000, 700], 2, 3, 128, 32, 8, 0, 1, seed=2, make=make)
+        for width in (0, 1025):
+            _select([300, 2000, 700], 2, 3, 128, 32, 8, 0, 1, seed=2, make=make, width=width)
 
 
 @pytest.mark.parametrize("dt", TYPES)

@@ -181,8 +181,11 @@ namespace dora {
 // some SIMDs two wavefronts and others one, is slower than both).  fp8 pages
 // take at most kFp8WavesPerCu: their per-page conversion work needs the
 // occupancy (4 per CU: 20% slower), and 7 per CU is 0.7% faster per step than
-// every resident slot (8).  Never more than the batch can use: at most
-// B * Hkv * stride page-heads, min_range each.
+// every resident slot (8).  4-bit pages take kFp4WavesPerCu, which are always
+// resident, so that the driver is not asked at each call (256 rows of 8 KV heads,
+// 1.7 GB: 286 us, with 2 a CU 364, with 5, 6 and 8 316, 300 and 303; 64 rows
+// of 4, 126 MB: 39.1 us, with 2, 6 and 8 43.2, 40.5 and 43.1).  Never more
+// than the batch can use: at most B * Hkv * stride page-heads, min_range each.
 int64_t decode_waves(const dora_decode_desc& d) {
   if (d.num_waves > 0) return d.num_waves;
   int dev = 0, cus = 0, per_cu = 0;
@@ -190,15 +193,14 @@ int64_t decode_waves(const dora_decode_desc& d) {
   const int seqs = d.num_seqs < kMaxSeqsPerLaunch ? d.num_seqs : kMaxSeqsPerLaunch;
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
-      (fp4 ? decode4_waves_per_cu(d.head_dim, d.page_size, seqs, &per_cu)
-           : decode_waves_per_cu(d.head_dim, d.page_size, fp8, seqs, &per_cu)) != hipSuccess ||
-      cus <= 0 || per_cu <= 0) {
+      (!fp4 && decode_waves_per_cu(d.head_dim, d.page_size, fp8, seqs, &per_cu) != hipSuccess) ||
+      cus <= 0 || (!fp4 && per_cu <= 0)) {
     (void)hipGetLastError();  // no device here: size for a 256-CU part at 8 waves per CU
     cus = 256;
     per_cu = 8;
   }
   const int cap = fp4 ? kFp4WavesPerCu : fp8 ? kFp8WavesPerCu : kBf16WavesPerCu;
-  if (per_cu > cap) per_cu = cap;
+  if (fp4 || per_cu > cap) per_cu = cap;  // (4-bit: always resident, and not asked for each call)
   const int64_t slots = (int64_t)cus * per_cu;
   // page-heads, or of 4-bit pages steps of 64 tokens
   const int64_t units =

@@ -2,6 +2,12 @@
 // tokens) work, as decode.hip has it over page-heads.  Every wavefront takes an equal
 // contiguous range; the pieces of the segments that the ranges cut are joined by decode.hip's
 // combine.
+//
+// Bound by memory, 17 / 32 byte a value: 256 rows of 8 KV heads (1.67 GB) 286 us with the combine, 5.9
+// TB/s; 64 rows of 4 KV heads (126 MB) 38.7 us, of which 6 are the combine and about 10 the
+// start: lengths, ids, first pages, one after another.  One wave a SIMD has 512 registers for two
+// steps of pages (17 KB) and its sums; a third step in flight was no faster (the loads of 1,024 waves, 18 MB,
+// already cover the latency), nor were more waves (api.cpp, decode_waves).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -215,11 +221,6 @@ static const void* decode4_symbol(int head_dim, int page_size) {
   if (head_dim == 128)
     return page_size == 16 ? (const void*)&decode4_kernel<128, 16, 2> : (const void*)&decode4_kernel<128, 32, 2>;
   return page_size == 16 ? (const void*)&decode4_kernel<64, 16, 2> : (const void*)&decode4_kernel<64, 32, 2>;
-}
-
-hipError_t decode4_waves_per_cu(int head_dim, int page_size, int num_seqs, int* out) {
-  return hipOccupancyMaxActiveBlocksPerMultiprocessor(out, decode4_symbol(head_dim, page_size), 64,
-                                                      decode_lds_bytes(num_seqs));
 }
 
 hipError_t launch_decode4(const DecodeParams& p, int head_dim, int page_size, int64_t waves,

@@ -10,8 +10,8 @@
 
 namespace dora {
 
-// Decode wavefronts per compute unit, at most, for bf16 and for fp8 pages (and
-// never more than the resident slots).  One equal range per wavefront.
+// Decode wavefronts per compute unit, at most, for bf16, for fp8 and for 4-bit
+// pages (and never more than the resident slots).  One equal range per wavefront.
 constexpr int kBf16WavesPerCu = 4;
 constexpr int kFp8WavesPerCu = 7;
 constexpr int kFp4WavesPerCu = 4;
@@ -214,7 +214,6 @@ hipError_t launch_decode(const DecodeParams& p, int head_dim, int page_size, boo
                          int64_t waves, hipStream_t s);
 // The stream-K decode of 4-bit pages (decode4.hip): DecodeParams' records and partials, its
 // work counted in steps of 64 tokens.
-hipError_t decode4_waves_per_cu(int head_dim, int page_size, int num_seqs, int* out);
 hipError_t launch_decode4(const DecodeParams& p, int head_dim, int page_size, int64_t waves,
                           hipStream_t s);
 hipError_t launch_segments(const SegmentParams& p, bool fp8, hipStream_t s);

@@ -2,7 +2,12 @@
 // names, or, of 4-bit pages without lists, all pages of a short row.
 //
 // Bound by memory: each listed page is read once, by one wave, straight into matrix operands
-// (16 query columns: a KV head's group), two steps of loads in flight.
+// (16 query columns: a KV head's group), two steps of loads in flight.  512 lists of 2,048 tokens in
+// bf16 (537 MB) take 86 us, 6.2 TB/s; 4,000 fp8 lists of up to 3,200 tokens (2.65 GB) 434 us, 6.1; 1,024
+// 4-bit lists of 2,560 tokens in pages of 16 (347 MB) 76 us, 4.6, in pages of 32 64 us, 5.5: a 4-bit
+// tile of 16 tokens and 128 dims is 1,088 bytes, half a line more than whole ones, and the rate of
+// tiles read here and there falls with their size.  Reading lists beside lengths and counts, one wait
+// fewer at the start, changed nothing: two or three workgroups a CU hide each other's start.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -302,27 +302,31 @@ __device__ __forceinline__ void as_operands(PageBounds<M>& x) {
   }
 }
 
-// A query row (of the lane's column `col`, a head of the group) as whole numbers, for the bytes that the lane has
-// of a page: max(u, 0) against the largest values, in the lower two lane groups, min(u, 0) against the
-// smallest in the upper two.
+// The rows of a group's 16 columns, D / 4 values of one a lane (row lane >> 2; rows that are none are 0).
 template <int D>
-struct ScoreQuery {
-  i32x4 w[D / 32];
-  float step;
+struct ScoreRows {
+  u32x4 w[D / 32];
 };
-
 template <int D>
-__device__ __forceinline__ void score_query(ScoreQuery<D>& s, const uint16_t* qrow, bool valid) {
-  const int grp = (threadIdx.x & 63) >> 4;
-  constexpr int N = D / 16;  // 8 values each
-  u32x4 w[N];
+__device__ __forceinline__ void load_rows(ScoreRows<D>& s, const uint16_t* group_rows, int group) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+    s.w[i] = lane >> 2 < group ? *(const u32x4*)(group_rows + (lane >> 2) * D + D / 4 * (lane & 3) + 8 * i)
+                               : u32x4{0u, 0u, 0u, 0u};
+}
+
+// The rows as whole numbers, into LDS: u[16][D], and their steps.
+template <int D>
+__device__ __forceinline__ void whole_rows(ScoreRows<D>& s, uint8_t* u, float* steps) {
+  const int lane = threadIdx.x & 63;
+  constexpr int N = D / 32;  // 8 values each
+  u32x4(&w)[N] = s.w;
   uint32_t most = 0;  // the largest magnitudes, two
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    w[i] = valid ? *(const u32x4*)(qrow + D / 2 * (grp & 1) + 8 * i) : u32x4{0u, 0u, 0u, 0u};
+  for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int k = 0; k < 4; ++k) most = max2(most, w[i][k] & 0x7FFF7FFFu);
-  }
   most = max2(most, most >> 16) & 0xFFFFu;
   const bool odd = most > 0x7F7Fu;  // a NaN or an infinity
   if (__ballot(odd)) {              // uniform, rare: each value for what it counts
@@ -338,12 +342,14 @@ __device__ __forceinline__ void score_query(ScoreQuery<D>& s, const uint16_t* qr
       }
     most = __float_as_uint(top) >> 16;
   }
-  const float top = max_xor16(__uint_as_float(most << 16));
-  s.step = fmaxf(__fdiv_rn(top, 127.0f), 0x1p-126f);
+  float top = __uint_as_float(most << 16);
+  top = fmaxf(top, __shfl_xor(top, 1));
+  top = fmaxf(top, __shfl_xor(top, 2));
+  float step = fmaxf(__fdiv_rn(top, 127.0f), 0x1p-126f);
+  if ((lane & 3) == 0) steps[lane >> 2] = step;
   // fp32(x / step): the product with the rounded reciprocal, corrected once by what it leaves, is
   // the rounded quotient (Markstein, "Computation of elementary functions on the IBM RISC System/6000
   // processor", 1990), as long as what is left is not below the normal numbers
-  float step = s.step;
   if (__ballot(step < 0x1p-90f)) {  // uniform, rare: the same quotients 2^64 higher up, exactly
     const float up = step < 0x1p-90f ? 0x1p64f : 1.f;
     step *= up;
@@ -355,23 +361,48 @@ __device__ __forceinline__ void score_query(ScoreQuery<D>& s, const uint16_t* qr
                   __float_as_uint(__uint_as_float(w[i][k] & 0xFFFF0000u) * up);
   }
   const float inverse = __fdiv_rn(1.0f, step);
+  uint8_t* to = u + (lane >> 2) * D + D / 4 * (lane & 3);
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m)
+  for (int i = 0; i < N; ++i) {
+    u32x2 eight;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 2; ++j) {
       uint32_t four = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t two = w[2 * m + (i >> 1)][2 * (i & 1) + (k >> 1)];
+        const uint32_t two = w[i][2 * j + (k >> 1)];
         const float x = __uint_as_float(k & 1 ? two & 0xFFFF0000u : two << 16);
         float y = x * inverse;
         y = __builtin_fmaf(__builtin_fmaf(-y, step, x), inverse, y);
-        const int u = (int)__builtin_rintf(y);  // (of at most 127.00001)
-        const int part = grp < 2 ? (u > 0 ? u : 0) : (u < 0 ? u : 0);
-        four |= (uint32_t)(part & 0xFF) << (8 * k);
+        four |= (uint32_t)((int)__builtin_rintf(y) & 0xFF) << (8 * k);  // (of at most 127.00001)
       }
-      s.w[m][i] = (int)four;
+      eight[j] = four;
     }
+    *(u32x2*)(to + 8 * i) = eight;
+  }
+}
+
+// The rows as an operand, for the bytes that a lane has of a page: max(u, 0) against the largest values, in the
+// lower two lane groups, min(u, 0) against the smallest in the upper two; and the steps of the rows
+// that the lane's results are.
+template <int D>
+struct ScoreQuery {
+  i32x4 w[D / 32];
+  f32x4 step;
+};
+template <int D>
+__device__ __forceinline__ void query_operand(ScoreQuery<D>& q, const uint8_t* u, const float* steps) {
+  const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+  q.step = *(const f32x4*)(steps + 4 * grp);
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m) {
+    q.w[m] = *(const i32x4*)(u + col * D + D / 2 * (grp & 1) + 16 * m);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = (uint32_t)q.w[m][i], negative = ((w >> 7) & 0x01010101u) * 0xFFu;
+      q.w[m][i] = (int)(grp < 2 ? w & ~negative : w & negative);
+    }
+  }
 }
 
 // The largest score of a page's over the group's rows, in all lanes of its column: sum and step are of
@@ -389,15 +420,16 @@ __device__ __forceinline__ float best_row(i32x4 sum, f32x4 step, int group) {
 // contiguous range, however long the sequences are.  By all threads of a workgroup; to: the range,
 // and the sequence and tile that it starts with.
 struct ScoreRange {
-  int count, b, tile;  // tiles of the range; where it starts
+  int count, b, tile, pages;  // tiles of the range; where it starts, and the pages of that sequence
 };
 __device__ __forceinline__ ScoreRange score_range(const SelectParams& p) {
   constexpr int THREADS = 64 * kScoreWaves;
-  __shared__ int s_wave[kScoreWaves], s_at[2];
+  __shared__ int s_wave[kScoreWaves], s_at[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = p.num_seqs;
-  auto tiles_of = [&](int b) { return (pages_of(p.seq_lens[b], p.page_size, p.stride) + 15) / 16; };
-  int sum = 0;
-  for (int b = tid; b < B; b += THREADS) sum += tiles_of(b);
+  auto pages_at = [&](int b) { return b < B ? pages_of(p.seq_lens[b], p.page_size, p.stride) : 0; };
+  const int own = pages_at(tid);
+  int sum = (own + 15) / 16;
+  for (int b = tid + THREADS; b < B; b += THREADS) sum += (pages_at(b) + 15) / 16;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
   if (lane == 0) s_wave[wave] = sum;
@@ -406,11 +438,11 @@ __device__ __forceinline__ ScoreRange score_range(const SelectParams& p) {
 #pragma unroll
   for (int w = 0; w < kScoreWaves; ++w) total += s_wave[w];
   const int x0 = (int)((int64_t)total * blockIdx.x / gridDim.x);
-  ScoreRange r{(int)((int64_t)total * (blockIdx.x + 1) / gridDim.x) - x0, 0, 0};
+  ScoreRange r{(int)((int64_t)total * (blockIdx.x + 1) / gridDim.x) - x0, 0, 0, 0};
   if (r.count == 0) return r;  // uniform
   int before = 0;
   for (int base = 0; base < B; base += THREADS) {
-    const int b = base + tid, n = b < B ? tiles_of(b) : 0;
+    const int b = base + tid, pages = base ? pages_at(b) : own, n = (pages + 15) / 16;
     int incl = n;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -430,6 +462,7 @@ __device__ __forceinline__ ScoreRange score_range(const SelectParams& p) {
     if (first <= x0 && x0 < last) {
       s_at[0] = b;
       s_at[1] = x0 - first;
+      s_at[2] = pages;
     }
     before += all;
     if (before > x0) break;  // uniform
@@ -437,6 +470,7 @@ __device__ __forceinline__ ScoreRange score_range(const SelectParams& p) {
   __syncthreads();
   r.b = uni(s_at[0]);
   r.tile = uni(s_at[1]);
+  r.pages = uni(s_at[2]);
   return r;
 }
 
@@ -448,41 +482,57 @@ __global__ __launch_bounds__(64 * kScoreWaves, kScorePerCu) void page_scores_ker
   constexpr int M = D / 32;
   __shared__ int s_id[kScoreMaxPages];
   __shared__ float s_out[kScoreWaves][2][kScoreMaxPages];  // (a store each time would be waited for with later loads)
+  __shared__ __align__(16) uint8_t s_u[kScoreWaves][2][16][D];
+  __shared__ __align__(16) float s_step[kScoreWaves][2][16];
   const int lane = threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
   const int Hkv = p.num_kv_heads, pairs = (Hkv + 1) / 2;
   const int ways = pairs == 1 ? 4 : pairs == 2 ? 2 : 1;  // waves that share a pair's tiles
   ScoreRange at = score_range(p);
   int held = -1;  // the sequence and pair whose rows are in q
   ScoreQuery<D> q[2];
+  auto hold_pair = [&](int pair, auto meanwhile) {
+    ScoreRows<D> rows[2];
+    const bool other = held != at.b * pairs + pair;  // uniform
+    if (other) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {  // (one head: the same again)
+        const int g = 2 * pair + h < Hkv ? 2 * pair + h : Hkv - 1;
+        load_rows<D>(rows[h], p.q + ((int64_t)at.b * p.num_q_heads + (int64_t)g * p.group) * D, p.group);
+      }
+    }
+    meanwhile();
+    if (!other) return;
+    held = at.b * pairs + pair;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int h = 0; h < 2; ++h) whole_rows<D>(rows[h], s_u[wave][h][0], s_step[wave][h]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int h = 0; h < 2; ++h) query_operand<D>(q[h], s_u[wave][h][0], s_step[wave][h]);
+  };
   while (at.count > 0) {  // uniform
-    const int n_seq = uni(pages_of(p.seq_lens[at.b], p.page_size, p.stride));
-    const int tiles = (n_seq + 15) / 16;
+    const int n_seq = at.pages, tiles = (n_seq + 15) / 16;
     if (at.tile >= tiles) {  // the next sequence
       ++at.b;
       at.tile = 0;
+      at.pages = uni(pages_of(p.seq_lens[at.b], p.page_size, p.stride));
       continue;
     }
     int n_tiles = tiles - at.tile < at.count ? tiles - at.tile : at.count;
     n_tiles = n_tiles < kScoreMaxPages / 16 ? n_tiles : kScoreMaxPages / 16;
     const int first = 16 * at.tile, n = n_seq - first < 16 * n_tiles ? n_seq - first : 16 * n_tiles;
-    __syncthreads();  // (s_id is read)
-    for (int i = threadIdx.x; i < n; i += blockDim.x)
-      s_id[i] = p.block_table[(int64_t)at.b * p.stride + first + i];
+    // the ids, and beside them the rows of the wave's first pair
+    static_assert(kScoreMaxPages == 64 * kScoreWaves, "an id a thread");
+    const int id = p.block_table[(int64_t)at.b * p.stride + first + ((int)threadIdx.x < n ? (int)threadIdx.x : n - 1)];
+    const int pair0 = wave / ways;
+    hold_pair(pair0 < pairs ? pair0 : 0, [&]() {
+      __syncthreads();  // (s_id is read)
+      s_id[threadIdx.x] = id;
+    });
     __syncthreads();
-    for (int pair = wave / ways; pair < pairs; pair += kScoreWaves / ways) {
+    for (int pair = pair0; pair < pairs; pair += kScoreWaves / ways) {
       const int g0 = 2 * pair, heads = Hkv - g0 < 2 ? 1 : 2;
-      if (held != at.b * pairs + pair) {  // uniform
-        held = at.b * pairs + pair;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          score_query<D>(q[h], p.q + ((int64_t)at.b * p.num_q_heads + (int64_t)(g0 + (h < heads ? h : 0)) * p.group + col) * D,
-                         col < p.group);
-      }
-      f32x4 step[2];  // of the rows that the lane's results are
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) step[h][k] = __shfl(q[h].step, 4 * grp + k);
+      if (pair != pair0) hold_pair(pair, []() {});
       // a tile's bounds; behind the last tile its loads are made again: under a branch they would be waited for
       // with those before them
       const int head2 = heads == 2 ? 2 * D : 0;  // (one head: the same again)
@@ -513,7 +563,7 @@ __global__ __launch_bounds__(64 * kScoreWaves, kScorePerCu) void page_scores_ker
 #pragma unroll
           for (int m = 0; m < M; ++m)
             sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[h].w[m], t.x[h].w[m], sum, 0, 0, 0);
-          best[h] = best_row(sum, step[h], p.group);
+          best[h] = best_row(sum, q[h].step, p.group);
         }
         if (grp < 2) s_out[wave][grp][16 * u + col] = (grp ? best[1] : best[0]) * t.s;
       };
@@ -783,7 +833,8 @@ __device__ __forceinline__ void score_row(const uint16_t* qrow, bool valid, uint
 template <int D>
 __global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(SelectParams p) {
   constexpr int M = D / 32, WAVES = kSelectThreads / 64, TILES = kSelectThreads / 16 / WAVES;
-  __shared__ float s_score[kSelectThreads], s_step[16];
+  __shared__ float s_score[kSelectThreads];
+  __shared__ __align__(16) float s_step[16];
   __shared__ __align__(16) uint8_t s_u[16][D];
   const int lane = threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
   const int Hkv = p.num_kv_heads, seg = blockIdx.x, b = seg / Hkv, g = seg - b * Hkv;
@@ -815,27 +866,16 @@ __global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(Selec
     s[k] = ((const float*)(page(col) + Hkv * (2 * D)))[g];
   }
   __syncthreads();
-  i32x4 q[M];
-  f32x4 step;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) step[k] = s_step[4 * grp + k];
-#pragma unroll
-  for (int m = 0; m < M; ++m) {
-    q[m] = *(const i32x4*)&s_u[col][D / 2 * (grp & 1) + 16 * m];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {  // the negative ones, or the others
-      const uint32_t w = (uint32_t)q[m][i], negative = ((w >> 7) & 0x01010101u) * 0xFFu;
-      q[m][i] = (int)(grp < 2 ? w & ~negative : w & negative);
-    }
-  }
+  ScoreQuery<D> q;
+  query_operand<D>(q, s_u[0], s_step);
 #pragma unroll
   for (int k = 0; k < TILES; ++k) {
     if (k >= mine) break;  // uniform
     as_operands<M>(x[k]);
     i32x4 sum{0, 0, 0, 0};
 #pragma unroll
-    for (int m = 0; m < M; ++m) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[m], x[k].w[m], sum, 0, 0, 0);
-    const float best = best_row(sum, step, p.group) * s[k];
+    for (int m = 0; m < M; ++m) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.w[m], x[k].w[m], sum, 0, 0, 0);
+    const float best = best_row(sum, q.step, p.group) * s[k];
     if (grp == 0) s_score[16 * (wave + k * WAVES) + col] = best;
   }
   __syncthreads();

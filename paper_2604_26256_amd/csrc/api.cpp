@@ -78,13 +78,12 @@ bool whole_segments(const dora_decode_desc& d, int64_t segs, int64_t tokens) {
 // The same choice for 4-bit pages: pages of a workgroup of the listed-pages kernel, which then
 // takes all pages of a row, or 0 for the stream-K decode.  A workgroup takes about 3.5 us and
 // 5.5 ns a token, the stream-K call and its combine 12-16 us however little there is to do.
-// So short rows go whole while the segments are few enough to be one or two launches' worth,
-// middle ones are cut where all their chunks run at once, and what is long and many is left to
-// the even ranges of the stream-K decode.  Over 3,824 batches of drawn shapes (up to 1,024
-// rows, 32,768 tokens, all lengths full, uniform, long-tailed or one long row) the rule takes
-// 0.70 of the stream-K decode's time and 1.02 of the best route's; a single long row among
-// short ones, which the table's width does not show, loses most (a row of 11,200 tokens and 15
-// short ones: 24.0 us, stream-K 14.2).
+// So short rows go whole, by one wave each where they are many, middle ones are cut where all their chunks
+// run at once, and what is long and many is left to the even ranges of the stream-K decode.
+// Over 3,264 batches of drawn shapes (up to 2,048 rows, 60,000 tokens, all lengths full, uniform,
+// long-tailed or one long row) the rule takes 0.69 of the stream-K decode's time and 1.02 of the
+// best route's; a single long row among short ones, which the table's width does not show,
+// loses most (a row of 11,200 tokens and 15 short ones: 24.0 us, stream-K 14.2).
 int pages4_split(const dora_decode_desc& d, int64_t segs, int64_t waves) {
   if (d.num_waves > 0 || d.min_range_pages > 0) return 0;
   const int64_t tokens = (int64_t)d.block_table_stride * d.page_size;
@@ -92,6 +91,7 @@ int pages4_split(const dora_decode_desc& d, int64_t segs, int64_t waves) {
     const int64_t workgroups = segs * ((tokens + chunk - 1) / chunk);
     return workgroups <= most && workgroups <= 2 * waves;
   };
+  if (pages4_waves(segs, tokens) == 1) return d.block_table_stride;
   if (tokens <= 1024) return segs <= 2048 ? d.block_table_stride : 0;
   if (fits(256, 256)) return 256 / d.page_size;
   if (tokens <= 2560 && segs <= 2048) return d.block_table_stride;
@@ -407,6 +407,9 @@ dora_status enqueue_decode(const dora_decode_desc& d, const void* q, const void*
       pp.list_stride = d.block_table_stride;
       pp.chunk_pages = seg_pages;
       pp.chunks = (d.block_table_stride + seg_pages - 1) / seg_pages;
+      pp.waves = pp.chunks > 1
+                     ? kSegWaves
+                     : pages4_waves(segs, (int64_t)d.block_table_stride * d.page_size);
       pp.scale_log2 = dp.scale_log2;
       if (launch_pages(pp, d.kv_dtype, s) != hipSuccess) return DORA_ERR_HIP;
       if (ev && c0 == 0 && hipEventRecord(ev[1], s) != hipSuccess) return DORA_ERR_HIP;

@@ -4,10 +4,10 @@
 // Bound by memory: each listed page is read once, by one wave, straight into matrix operands
 // (16 query columns: a KV head's group), two steps of loads in flight.  512 lists of 2,048 tokens in
 // bf16 (537 MB) take 86 us, 6.2 TB/s; 4,000 fp8 lists of up to 3,200 tokens (2.65 GB) 434 us, 6.1; 1,024
-// 4-bit lists of 2,560 tokens in pages of 16 (347 MB) 76 us, 4.6, in pages of 32 64 us, 5.5: a 4-bit
+// 4-bit lists of 2,560 tokens in pages of 16 (347 MB) 70 us, 4.9, where pages of 32 reach 5.5: a 4-bit
 // tile of 16 tokens and 128 dims is 1,088 bytes, half a line more than whole ones, and the rate of
 // tiles read here and there falls with their size.  Reading lists beside lengths and counts, one wait
-// fewer at the start, changed nothing: two or three workgroups a CU hide each other's start.
+// fewer at the start, changed nothing: what runs beside a start hides it.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -53,15 +53,15 @@ __device__ __forceinline__ void pages_stage(const PagesParams& p, PagesStage& s,
 
 // What a wave holds of a segment after its pages, into LDS; then the workgroup's merge of its
 // waves, and the output rows or, where the segment has further chunks, a partial.
-template <int D>
+template <int D, int WAVES>
 struct PagesMerge {
-  float o[kSegWaves][16][D + 4];
-  float2 ml[kSegWaves][16];
-  int any[kSegWaves];  // whether a token counted
+  float o[WAVES][16][D + 4];
+  float2 ml[WAVES][16];
+  int any[WAVES];  // whether a token counted
 };
 
-template <int D>
-__device__ __forceinline__ void pages_finish(const PagesParams& p, PagesMerge<D>& s,
+template <int D, int WAVES>
+__device__ __forceinline__ void pages_finish(const PagesParams& p, PagesMerge<D, WAVES>& s,
                                              const f32x4 (&acc)[D / 16], float m_run, float l_run,
                                              bool any, int seg, int64_t row0, int c, bool cut) {
   const int lane = threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6);
@@ -76,16 +76,16 @@ __device__ __forceinline__ void pages_finish(const PagesParams& p, PagesMerge<D>
   __syncthreads();
   bool some = false;
 #pragma unroll
-  for (int w = 0; w < kSegWaves; ++w) some = some || s.any[w];
-  for (int e = threadIdx.x; e < G * (D / 4); e += 64 * kSegWaves) {
+  for (int w = 0; w < WAVES; ++w) some = some || s.any[w];
+  for (int e = threadIdx.x; e < G * (D / 4); e += 64 * WAVES) {
     const int h = e / (D / 4), d4 = e - h * (D / 4);
     float M = kNoMax, S = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kSegWaves; ++w)
+    for (int w = 0; w < WAVES; ++w)
       if (s.any[w]) M = fmaxf(M, s.ml[w][h].x);
 #pragma unroll
-    for (int w = 0; w < kSegWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (!s.any[w]) continue;
       const float2 ml = s.ml[w][h];
       const float f = ml.x == M ? 1.f : __builtin_amdgcn_exp2f(ml.x - M);
@@ -105,14 +105,14 @@ __device__ __forceinline__ void pages_finish(const PagesParams& p, PagesMerge<D>
   }
 }
 
-// One workgroup of kSegWaves waves per (sequence, KV head) segment, or per chunk of
+// One workgroup of WAVES waves per (sequence, KV head) segment, or per chunk of
 // p.chunk_pages of its listed pages.  bf16 and fp8 pages; a step is one page.
-template <int D, int P, bool FP8>
-__global__ __launch_bounds__(64 * kSegWaves, 2) void pages_kernel(PagesParams p) {
+template <int D, int P, bool FP8, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void pages_kernel(PagesParams p) {
   constexpr int DBLK = D / 16, TILE_BYTES = P * D * (FP8 ? 1 : 2);
   __shared__ __align__(16) union {
     PagesStage stage;
-    PagesMerge<D> merge;
+    PagesMerge<D, WAVES> merge;
   } s;
   const int lane = threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6);
   const int col = lane & 15, grp = lane >> 4;
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void pages_kernel(PagesParams p)
   for (int i = 0; i < DBLK; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = kNoMax, l_run = 0.f;
   bool any = false;
-  const int steps = (n - wave + kSegWaves - 1) / kSegWaves;  // <= 0: none for this wave
+  const int steps = (n - wave + WAVES - 1) / WAVES;  // <= 0: none for this wave
   if (steps > 0) {
     const uint32_t koff = step_koff<D, P, P>(col, grp), voff = step_voff<D, P, FP8, P>(col, grp);
     PageRegs<D, P, FP8> buf[2];
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(64 * kSegWaves, 2) void pages_kernel(PagesParams p)
     int tokens[2];
     auto prefetch = [&](int r, int u) {
       const bool past = u >= steps;  // past the last step the loads still issue, one line each
-      const int i = wave + kSegWaves * (past ? steps - 1 : u);
+      const int i = wave + WAVES * (past ? steps - 1 : u);
       const int page = uni(s.stage.id[i]);
       tokens[r] = uni(s.stage.tokens[i]);
       if constexpr (FP8) {
@@ -176,13 +176,13 @@ done:
 }
 
 // The same over 4-bit pages; a step is 64 tokens.
-template <int D, int P>
-__global__ __launch_bounds__(64 * kSegWaves, 3) void pages4_kernel(PagesParams p) {
+template <int D, int P, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 3) void pages4_kernel(PagesParams p) {
   typedef Fp4<D, P> F;
   constexpr int DBLK = D / 16;
   __shared__ __align__(16) union {
     PagesStage stage;
-    PagesMerge<D> merge;
+    PagesMerge<D, WAVES> merge;
   } s;
   __shared__ bf16x8 s_q[D / 32][64];
   const int lane = threadIdx.x & 63, wave = uni((int)threadIdx.x >> 6);
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(64 * kSegWaves, 3) void pages4_kernel(PagesParams p
   float m_run = kNoMax, l_run = 0.f;
   bool any = false;
   const int n_steps = (n + F::PAGES - 1) / F::PAGES;
-  const int steps = (n_steps - wave + kSegWaves - 1) / kSegWaves;
+  const int steps = (n_steps - wave + WAVES - 1) / WAVES;
   if (steps > 0) {
     const uint32_t koff = F::k_off(lane), ksoff = F::k_scale_off(lane), voff = F::v_off(lane),
                    vsoff = F::v_scale_off(lane);
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(64 * kSegWaves, 3) void pages4_kernel(PagesParams p
     int nv[2];
     auto prefetch = [&](int r, int u) {
       // (past the last step it is loaded again: under a branch the loads would be waited for together)
-      const int i = F::PAGES * (wave + kSegWaves * (u < steps ? u : steps - 1)), last = n - 1;
+      const int i = F::PAGES * (wave + WAVES * (u < steps ? u : steps - 1)), last = n - 1;
       const int ik = i + F::k_page(lane), iv = i + F::v_page(lane);  // past the end: no tokens
       const int64_t k = s.stage.id[ik < n ? ik : last], v = s.stage.id[iv < n ? iv : last];
       nv[r] = iv < n ? s.stage.tokens[iv] - F::group_slot(lane) : 0;
@@ -288,21 +288,26 @@ __global__ __launch_bounds__(256) void pages_validate_kernel(ValidateParams p, c
   }
 }
 
-template <int D, int P>
+template <int D, int P, int WAVES>
 static const void* pages_fn(int kv_dtype) {
-  return kv_dtype == DORA_KV_FP4        ? (const void*)&pages4_kernel<D, P>
-         : kv_dtype == DORA_KV_FP8_E4M3 ? (const void*)&pages_kernel<D, P, true>
-                                        : (const void*)&pages_kernel<D, P, false>;
+  return kv_dtype == DORA_KV_FP4        ? (const void*)&pages4_kernel<D, P, WAVES>
+         : kv_dtype == DORA_KV_FP8_E4M3 ? (const void*)&pages_kernel<D, P, true, WAVES>
+                                        : (const void*)&pages_kernel<D, P, false, WAVES>;
+}
+template <int WAVES>
+static const void* pages_fn(int kv_dtype, int head_dim, int page_size) {
+  return head_dim == 128
+             ? (page_size == 16 ? pages_fn<128, 16, WAVES>(kv_dtype) : pages_fn<128, 32, WAVES>(kv_dtype))
+             : (page_size == 16 ? pages_fn<64, 16, WAVES>(kv_dtype) : pages_fn<64, 32, WAVES>(kv_dtype));
 }
 
 hipError_t launch_pages(const PagesParams& p, int kv_dtype, hipStream_t s) {
-  const void* fn =
-      p.head_dim == 128 ? (p.page_size == 16 ? pages_fn<128, 16>(kv_dtype) : pages_fn<128, 32>(kv_dtype))
-                        : (p.page_size == 16 ? pages_fn<64, 16>(kv_dtype) : pages_fn<64, 32>(kv_dtype));
+  const void* fn = p.waves == 1 ? pages_fn<1>(kv_dtype, p.head_dim, p.page_size)
+                                : pages_fn<kSegWaves>(kv_dtype, p.head_dim, p.page_size);
   PagesParams arg = p;
   void* args[] = {(void*)&arg};
   return hipLaunchKernel(fn, dim3((unsigned)(p.num_seqs * p.num_kv_heads), (unsigned)p.chunks),
-                         dim3(64 * kSegWaves), args, 0, s);
+                         dim3(64u * (unsigned)p.waves), args, 0, s);
 }
 
 hipError_t launch_pages_combine(const PagesParams& p, hipStream_t s) {

@@ -31,6 +31,7 @@ struct PagesParams {
   int32_t list_stride;
   int32_t chunk_pages;    // listed pages of a workgroup
   int32_t chunks;         // workgroups of a segment
+  int32_t waves;          // of a workgroup: kSegWaves or 1
   float scale_log2;
 };
 hipError_t launch_pages(const PagesParams& p, int kv_dtype, hipStream_t s);
@@ -72,6 +73,26 @@ inline void pages_layout(const dora_decode_desc& d, int32_t list_stride, PagesLa
   w->part_o_off = kWsHeaderBytes;
   w->part_ml_off = up(w->part_o_off + slots * G * d.head_dim * 4);
   w->total = up(w->part_ml_off + slots * G * 8);
+}
+
+// Waves of a workgroup that has a whole list of at most `tokens`.  With one, four times as many lists are
+// under way and none is merged, but a list's steps follow each other: so for short lists of many
+// segments, and of 4-bit pages (64 tokens a step) for all where the segments are two to a CU.
+// Over 1,090 drawn batches of lists of 16 to 4,096 tokens this takes 1.01 of the better one's time,
+// four waves always 1.16 for 4-bit pages, 1.07 for bf16 and 1.06 for fp8 (8,000 4-bit lists of 32
+// tokens: 47 and 21 us; 1,024 of 2,560: 75.8 and 69.8; 4,000 fp8 lists of up to 3,200: 434 and 480).
+inline int pages_waves(const dora_decode_desc& d, int64_t segs, int64_t tokens) {
+  const bool one = d.kv_dtype == DORA_KV_FP4
+                       ? (tokens <= 64 && segs >= 128) || (tokens <= 4096 && segs >= 512)
+                       : (tokens <= 32 && segs >= 128) || (tokens <= 256 && segs >= 640);
+  return one ? 1 : kSegWaves;
+}
+
+// The same for the 4-bit decode, whose rows (at most `tokens`, the table's width) are less even.
+inline int pages4_waves(int64_t segs, int64_t tokens) {
+  const bool one = (tokens <= 128 && segs >= 256) || (tokens <= 768 && segs >= 640) ||
+                   (tokens <= 1536 && segs >= 2048);
+  return one ? 1 : kSegWaves;
 }
 
 // Bytes of a page's bounds: int8 [Hkv][2][d] (largest, smallest), fp32 [Hkv] scales.

@@ -15,7 +15,7 @@
 //
 // Bounds are bound by memory and, in small calls, by their start: 1,024 rows' newest page, 8 bf16 heads (19 MB) 9.4
 // us, 24 fp8 prompts of 900 to 1,900 tokens (37 MB) 11.9.  Scores: 64 long rows, 8 heads (338 MB of
-// bounds) 76 us, 4.5 TB/s.  Without the products they take as long: a record of 2,080 bytes lies on
+// bounds) 71 us, 4.8 TB/s.  Without the products they take as long: a record of 2,080 bytes lies on
 // 17.1 lines of 128 on average, and no more is gained by 2 workgroups a CU, or loads past the L2 (4 spill).  Their
 // choice then takes 12, a row's passes over its scores one after another.
 #include <hip/hip_runtime.h>
@@ -886,10 +886,11 @@ __global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(Selec
   if (!all) choose_pages<1>(p, n, list, [&](int i) { return s_score[i]; });
 }
 
-// One launch takes 5.5 to 8 us for rows of up to 256 pages and 12 for 1,024, two take 12.5 to 24, as long
-// as a round of workgroups (one of 16 waves on a CU) has the batch; of short rows, two rounds are worth it
-// too (64 rows, 8 KV heads, 256 pages: 18.9 and 26.3 us; 1,024 pages: 48.4 and 37.2, as bounds
-// are read best with all heads of a page at once, which page_scores_kernel does).
+// One launch takes 6 to 9 us for rows of up to 256 pages and 12 to 25 for 1,024, two take 11 to 18 and 15
+// to 24, as long as a round of workgroups (one of 16 waves on a CU) has the batch; of short rows, two
+// rounds are worth it too (64 rows, 8 KV heads, 128 pages: 13.1 and 15.9 us, 256 pages 19.1 and 19.7; 1,024
+// pages 47.9 and 34.5, as bounds are read best with all heads of a page at once, which
+// page_scores_kernel does).
 bool select_at_once(const SelectParams& p, int cus) {
   const int64_t segs = (int64_t)p.num_seqs * p.num_kv_heads;
   return p.stride <= 256 ? segs <= 2 * cus : p.stride <= kSelectThreads && segs <= cus;

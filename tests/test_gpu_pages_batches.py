@@ -8,7 +8,7 @@ from cache_util import bound, check
 from fp4_util import FP4, Cache4, bf16_of, bf16_value, dec4, key_codes, make_cache, value_codes
 from gpu_util import lib
 from test_gpu_fp4 import _reference as _dense_reference
-from test_gpu_pages import TYPES, _q, _reference
+from test_gpu_pages import LENS, TYPES, _hide, _lists, _q, _reference
 from test_gpu_select import _bounds, _record, _tokens32
 
 pytestmark = pytest.mark.gpu
@@ -73,6 +73,26 @@ def test_more_sequences_than_a_launch_covers(dt, B):
     assert e.value.status == D.DORA_ERR_DEVICE_CHECK
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("P", [16, 32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,width", [(1, 1), (4, 3), (16, 8), (7, 150)])
+def test_lists_of_many_segments(dt, P, d, G, width):
+    """As many lists as make a wave each the better way where they are short."""
+    print(f"[case] many lists dt={dt} P={P} d={d} G={G} width={width}", flush=True)
+    c = make_cache(LENS, 2, d, P, dt, seed=width)
+    q = _q(len(LENS), 2 * G, d, G)
+    lists, counts = _lists(np.random.default_rng(G + width), c, width, 2)
+    want, spread = _reference(c, q, lists, counts)
+    _hide(c, lists, counts)
+    dev, at = _tiled(c, 330)
+    out = torch.full((330, 2 * G, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    lib().dora_decode_attn_pages(q[at].cuda().contiguous(), torch.from_numpy(lists)[at].cuda().contiguous(),
+                                 torch.from_numpy(counts)[at].cuda().contiguous(), dev["k"], dev["v"], dev["bt"], dev["lens"], None, out,
+                                 **dev["kw"])
+    _check_tiled(out, at, want, spread, "pages")
+
+
 @pytest.mark.parametrize("one", [False, True])
 def test_stores_and_reads_of_more_sequences_than_a_launch_covers(one):
     """33,000 sequences with a page of their own: stored bit for bit as their rows say, read back, and bounded."""
@@ -108,9 +128,9 @@ def test_stores_and_reads_of_more_sequences_than_a_launch_covers(one):
     assert np.array_equal(seen, top)
 
 
-ROUTES = [  # rows, KV heads, longest row, pages of 16 tokens in a workgroup: whole rows, chunks, and none
+ROUTES = [  # rows, KV heads, longest row, pages of 16 tokens in a workgroup: whole rows (None), chunks, and 0
     (5, 2, 900, None), (2000, 1, 60, None), (5, 2, 1500, 16), (100, 2, 2300, None), (6, 2, 6000, 32), (40, 1, 4500, 64), (12, 2, 15000, 64),
-    (3, 1, 32000, 32), (300, 2, 2700, 0), (1100, 2, 200, 0)]
+    (3, 1, 32000, 32), (300, 2, 2700, 0), (1100, 2, 200, None), (700, 1, 740, None), (400, 8, 1500, None), (400, 8, 1600, 0)]
 
 
 @pytest.mark.parametrize("B,Hkv,longest,pages", ROUTES)

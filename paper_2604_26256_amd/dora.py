@@ -265,19 +265,21 @@ def _k_geometry(k_pages, num_kv_heads, page_size, head_dim, kv_dtype):
         if head_dim % X:
             raise ValueError("head_dim must be a multiple of 16 bytes of elements")
         tail = (num_kv_heads, head_dim // X, page_size, X)
-    if k_pages.shape[1:] != tail:
-        raise ValueError(f"k_pages must be [num_pages]{list(tail)}, got {list(k_pages.shape)}")
+    shape = k_pages.shape
+    num_pages = shape[0] if len(shape) else -1
+    if shape != (num_pages, *tail):  # (one comparison of whole shapes: a slice of one takes 0.4 us)
+        raise ValueError(f"k_pages must be [num_pages]{list(tail)}, got {list(shape)}")
     kv_types = ((torch.bfloat16,) if kv_dtype == DORA_KV_BF16 else (torch.uint8,)
                 if kv_dtype == DORA_KV_FP4 else (torch.uint8, torch.float8_e4m3fn))
-    return int(k_pages.shape[0]), kv_types
+    return num_pages, kv_types
 
 
 def _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, head_dim, kv_dtype):
     num_pages, kv_types = _k_geometry(k_pages, num_kv_heads, page_size, head_dim, kv_dtype)
-    tail = (tuple(k_pages.shape[1:]) if kv_dtype == DORA_KV_FP4
-            else (num_kv_heads, head_dim, page_size))
-    if v_pages.shape[1:] != tail or v_pages.shape[0] != num_pages:
-        raise ValueError(f"v_pages must be [num_pages]{list(tail)}, got {list(v_pages.shape)}")
+    want = (k_pages.shape if kv_dtype == DORA_KV_FP4
+            else (num_pages, num_kv_heads, head_dim, page_size))
+    if v_pages.shape != want:
+        raise ValueError(f"v_pages must be [num_pages]{list(want[1:])}, got {list(v_pages.shape)}")
     return num_pages, kv_types
 
 
@@ -943,7 +945,7 @@ def dora_page_bounds_bytes(num_kv_heads, head_dim) -> int:
 
 
 def _bounds_shape(num_pages, num_kv_heads, head_dim):
-    return num_pages, dora_page_bounds_bytes(num_kv_heads, head_dim)
+    return num_pages, _lib.dora_page_bounds_bytes(num_kv_heads, head_dim)
 
 
 def dora_kv_page_bounds(k_pages, block_table, seq_lens, bounds, *, num_tokens, head_dim, num_kv_heads,

@@ -9,7 +9,7 @@ from fp4_util import FP4, Cache4, bf16_of, bf16_value, dec4, key_codes, make_cac
 from gpu_util import lib
 from test_gpu_fp4 import _reference as _dense_reference
 from test_gpu_pages import LENS, TYPES, _hide, _lists, _q, _reference
-from test_gpu_select import _bounds, _record, _tokens32
+from test_gpu_select import _bounds, _record, _select, _tokens32
 
 pytestmark = pytest.mark.gpu
 
@@ -200,3 +200,85 @@ def test_two_graphs_on_two_streams():
         torch.cuda.synchronize()
         for _, _, _, outs, eager in runs:
             assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_far_pages_are_read_as_near_ones(dt):
+    """The same pages within 4 GB of the pool's start and behind: reads, bounds, attention over lists (four waves and one a
+    list) and, of 4-bit pages, the decode by ranges are equal bit for bit."""
+    D, Hkv, d, P = lib(), 2, 128, 32
+    c = make_cache([900, 33, 0, 257], Hkv, d, P, dt, seed=9)
+    near = c.gpu()
+    page = near["k"][0].numel() * near["k"].element_size()
+    far = (1 << 32) // page + 5  # the first page that begins behind 4 GB
+    pool = {}
+    for n in "kv":
+        big = torch.empty((far + c.num_pages, *near[n].shape[1:]), dtype=near[n].dtype, device="cuda")
+        big[far:] = near[n]
+        pool[n] = big
+    kw = dict(near["kw"])
+    if dt == 1:
+        for n in ("k_scales", "v_scales"):
+            kw[n] = torch.cat([torch.full((far,), float("nan"), device="cuda"), near["kw"][n]])
+    bt = (near["bt"] + far).contiguous()
+    lens = near["lens"]
+    rec = D.dora_page_bounds_bytes(Hkv, d)
+    bounds = [torch.zeros(n, rec, dtype=torch.uint8, device="cuda") for n in (c.num_pages, far + c.num_pages)]
+    rows = [[torch.zeros(4, 900, Hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2)]
+    for i, (k, v, t, w) in enumerate(((near["k"], near["v"], near["bt"], near["kw"]), (pool["k"], pool["v"], bt, kw))):
+        D.dora_kv_read(k, v, t, lens, *rows[i], counts=lens, **w)
+        D.dora_kv_page_bounds(k, t, lens, bounds[i], num_tokens=900, head_dim=d, counts=lens, **{n: x for n, x in w.items() if n != "v_scales"})
+    assert torch.equal(bounds[0], bounds[1][far:])
+    for a, b in zip(*rows):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+    for B in (4, 330):
+        at = (torch.arange(B) % 4).cuda()
+        q = _q(4, Hkv * 3, d, 2).cuda()[at].contiguous()
+        lists = torch.arange(6, dtype=torch.int32, device="cuda").repeat(B, Hkv, 1).contiguous()
+        counts = torch.full((B, Hkv), 6, dtype=torch.int32, device="cuda")
+        outs = [torch.zeros_like(q) for _ in range(4)]
+        D.dora_decode_attn_pages(q, lists, counts, near["k"], near["v"], near["bt"][at].contiguous(), lens[at].contiguous(), None, outs[0], **near["kw"])
+        D.dora_decode_attn_pages(q, lists, counts, pool["k"], pool["v"], bt[at].contiguous(), lens[at].contiguous(), None, outs[1], **kw)
+        D.dora_decode_attn(q, near["k"], near["v"], near["bt"][at].contiguous(), lens[at].contiguous(), None, outs[2], num_waves=9, **near["kw"])
+        D.dora_decode_attn(q, pool["k"], pool["v"], bt[at].contiguous(), lens[at].contiguous(), None, outs[3], num_waves=9, **kw)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[2], outs[3]) and not outs[0].isnan().any()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_as_many_kv_heads_as_there_may_be(dt):
+    """127 KV heads: waves of a workgroup take several, the choice its last pair alone."""
+    D, Hkv, d, P = lib(), 127, 64, 16
+    c = make_cache([40, 0, 17], Hkv, d, P, dt, seed=2)
+    dev = c.gpu()
+    bounds = torch.zeros(c.num_pages, D.dora_page_bounds_bytes(Hkv, d), dtype=torch.uint8, device="cuda")
+    D.dora_kv_page_bounds(dev["k"], dev["bt"], dev["lens"], bounds, num_tokens=40, head_dim=d, counts=dev["lens"],
+                          **{n: x for n, x in dev["kw"].items() if n != "v_scales"})
+    for b, j in ((0, 0), (0, 2), (2, 1)):
+        t = np.arange(j * P, min(int(c.lens[b]), (j + 1) * P))
+        used = Hkv * (2 * d + 4)
+        assert np.array_equal(bounds[int(c.bt[b, j])].cpu().numpy()[:used], _record(*_bounds(_tokens32(c, b, t)))[:used])
+    out = [torch.zeros(3, 40, Hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    D.dora_kv_read(dev["k"], dev["v"], dev["bt"], dev["lens"], *out, counts=dev["lens"], **dev["kw"])
+    for b, L in enumerate(c.lens):
+        for x, y in zip(out, c.tokens(b, np.arange(L))):
+            assert np.array_equal(x[b, :L].cpu().view(torch.int16).numpy().view(np.uint16), bf16_of(y))
+    q = _q(3, Hkv * 2, d, 4)
+    lists = np.tile(np.array([2, 0], np.int32), (3, Hkv, 1))
+    counts = np.full((3, Hkv), 2, np.int32)
+    want, spread = _reference(c, q, lists, counts)
+    got = torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+    D.dora_decode_attn_pages(q.cuda(), torch.from_numpy(lists).cuda(), torch.from_numpy(counts).cuda(), dev["k"], dev["v"], dev["bt"],
+                             dev["lens"], None, got, **dev["kw"])
+    check(got, want, spread, "pages")
+    if dt == FP4:
+        for waves in (0, 40):
+            D.dora_decode_attn(q.cuda(), dev["k"], dev["v"], dev["bt"], dev["lens"], None, got, num_waves=waves, **dev["kw"])
+            check(got, *_dense_reference(c, q), "decode4")
+        k, v = torch.full_like(dev["k"], 0xFF), torch.full_like(dev["v"], 0xFF)
+        D.dora_kv_append_path(*out, dev["bt"], dev["lens"], k, v, counts=dev["lens"], **dev["kw"])
+        again = [torch.zeros_like(x) for x in out]
+        D.dora_kv_read(k, v, dev["bt"], dev["lens"], *again, counts=dev["lens"], **dev["kw"])
+        # a block's largest K is at least 4 steps and at most 6, so that K's values are stored again as they are
+        assert torch.equal(out[0].view(torch.int16), again[0].view(torch.int16))
+    for width in (0, 1025):
+        _select([300, 77, 0], Hkv, 1, d, P, 5, 1, 1, seed=3, width=width)

@@ -133,10 +133,9 @@ def test_all_pages_listed_is_the_plain_decode(dt, P, d):
     width = c.bt.shape[1]
     lists = np.tile(np.arange(width, dtype=np.int32), (6, 2, 1))
     counts = np.tile((-(-c.lens // P))[:, None], (1, 2)).astype(np.int32)
-    out = _run(c, q.cpu(), lists, counts)
-    a, b = out.float(), plain.float()
-    # both are within half a step of the same sums, whose weights are rounded alike but for their reference
-    assert float((a - b).abs().max()) <= 2 * 2.0 ** -8 * float(b.abs().max())
+    want, spread = _reference(c, q.cpu(), lists, counts)
+    check(_run(c, q.cpu(), lists, counts), want, spread, "pages")
+    check(plain, want, spread, "plain decode")
 
 
 @pytest.mark.parametrize("dt", TYPES)

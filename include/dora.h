@@ -193,7 +193,10 @@ int64_t dora_decode_num_waves(const dora_decode_desc* desc);
  * 512-2,048 tokens), or one per chunk of 256 or 512 tokens of it and a combine (rows
  * from 768 tokens on); dora_decode_segment_pages in dora_measure.h tells which.
  * Results do not depend on the number of wavefronts beyond fp32 rounding, and
- * repeated calls on the same inputs and device are bitwise identical. */
+ * repeated calls on the same inputs and device are bitwise identical.
+ * Scores and sums are held in fp32.  Of 4-bit pages any finite values give a finite
+ * result; of bf16 and fp8 pages the magnitudes of the values that a row attends, each
+ * times its weight relative to the row's largest, have to add up to less than 2^128. */
 dora_status dora_decode_attn(const dora_decode_desc* desc,
                              const void* q, const void* k_pages, const void* v_pages,
                              const int32_t* block_table, const int32_t* seq_lens,

@@ -125,7 +125,13 @@ struct Fp4 {
   // slots hold is not used: a code is finite whatever it is, and scores and scales are replaced.
   //   m_run is a reference and not the running maximum: it moves only where a lane's weights sum to more than
   // kMostWeight, so that most steps neither look for their maximum nor rescale.
+  //   What a row adds up stays below 2^128, whatever finite values it attends (and scores up to 2^24, from which on
+  // fp32 holds no units of them): a lane's 16 weights sum to 2^8 at
+  // most, so a row of up to 2^24 tokens adds at most 2^28 times 6 kFarScale, 2^126.6, for the steps whose V scales
+  // are up to that; a step with a larger one has its reference kFarMargin above its largest score, so that such
+  // tokens' weights are 2^-32 at most and add 2^24 * 2^-32 * 2^128.
   static constexpr float kMostWeight = 256.f;
+  static constexpr float kFarScale = 0x1p96f, kFarMargin = 32.f;
   template <typename QueryAt>
   static __device__ __forceinline__ void consume(const Regs& r, bool all, int nv, float mul, QueryAt q,
                                                  f32x4 (&acc)[D / 16], float& m_run, float& l_run) {
@@ -168,13 +174,15 @@ struct Fp4 {
         }
     };
     weigh();
-    if (__ballot(!(sum <= kMostWeight))) {  // uniform
+    const bool far = fmaxf(scale[0], scale[D / 64 - 1]) > kFarScale;
+    if (__ballot(far || !(sum <= kMostWeight))) {  // uniform
+      const float margin = __ballot(far) ? kFarMargin : 0.f;
       float mx = -__builtin_inff();
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[t][i]);
-      const float m_new = fmaxf(m_run, mul * max_xor32(max_xor16(mx)));
+      const float m_new = fmaxf(m_run, __builtin_fmaf(mul, max_xor32(max_xor16(mx)), margin));
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;

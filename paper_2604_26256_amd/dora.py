@@ -909,6 +909,8 @@ def dora_kv_read(k_pages, v_pages, block_table, seq_lens, k_out, v_out, *, num_k
     """Read the last counts[b] (T without counts) tokens of each sequence into rows of k_out and
     v_out (bf16 [B][T][Hkv][d]); see include/dora.h."""
     torch = _torch()
+    if k_pages is None or v_pages is None or block_table is None or k_out is None:
+        _need(k_pages=k_pages, v_pages=v_pages, block_table=block_table, k_out=k_out)
     if k_out.dim() != 4 or k_out.shape[2] != num_kv_heads:
         raise ValueError("k_out must be [B][T][num_kv_heads][head_dim]")
     B, T, _, D = k_out.shape
@@ -955,6 +957,10 @@ def dora_kv_page_bounds(k_pages, block_table, seq_lens, bounds, *, num_tokens, h
     counts[b] (num_tokens without counts) tokens of a sequence lie in; see include/dora.h."""
     torch = _torch()
     num_tokens = _i32("num_tokens", num_tokens)
+    if k_pages is None or block_table is None or seq_lens is None:
+        _need(k_pages=k_pages, block_table=block_table, seq_lens=seq_lens)
+    if seq_lens.dim() != 1:
+        raise ValueError("seq_lens must be [B]")
     B = seq_lens.shape[0]
     num_pages, kv_types = _k_geometry(k_pages, num_kv_heads, page_size, head_dim, kv_dtype)
     if kv_dtype != DORA_KV_FP8_E4M3:
@@ -993,6 +999,8 @@ def dora_page_select(q, bounds, block_table, seq_lens, page_lists, page_counts, 
     first sink_pages and the last recent_pages are always among them.  q: bf16 [B][Hq][d]; bounds:
     as dora_kv_page_bounds writes them; scores: optional fp32 [B][Hkv][stride]."""
     torch = _torch()
+    if q is None or bounds is None or block_table is None or page_lists is None:
+        _need(q=q, bounds=bounds, block_table=block_table, page_lists=page_lists)
     if q.dim() != 3:
         raise ValueError("q must be [B][num_q_heads][head_dim]")
     B, Hq, D = q.shape
@@ -1000,6 +1008,8 @@ def dora_page_select(q, bounds, block_table, seq_lens, page_lists, page_counts, 
         raise ValueError("block_table must be [B][stride]")
     if page_lists.dim() != 3:
         raise ValueError("page_lists must be [B][num_kv_heads][budget]")
+    if bounds.dim() != 2:
+        raise ValueError("bounds must be [num_pages][dora_page_bounds_bytes]")
     stride, budget = block_table.shape[1], page_lists.shape[2]
     desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
                             page_size=page_size, block_table_stride=max(1, stride),
@@ -1038,6 +1048,8 @@ def dora_decode_attn_pages(q, page_lists, page_counts, k_pages, v_pages, block_t
     [B][Hkv][list_stride], numbers of a sequence's pages, of which page_counts int32 [B][Hkv]
     are listed.  Other arguments as for dora_decode_attn.  Returns `out`."""
     torch = _torch()
+    if q is None or k_pages is None or v_pages is None or block_table is None or page_lists is None:
+        _need(q=q, k_pages=k_pages, v_pages=v_pages, block_table=block_table, page_lists=page_lists)
     if q.dim() != 3:
         raise ValueError("q must be [B][num_q_heads][head_dim]")
     B, Hq, D = q.shape

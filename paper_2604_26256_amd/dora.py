@@ -1008,7 +1008,7 @@ def dora_page_select(q, bounds, block_table, seq_lens, page_lists, page_counts, 
         raise ValueError("block_table must be [B][stride]")
     if page_lists.dim() != 3:
         raise ValueError("page_lists must be [B][num_kv_heads][budget]")
-    if bounds.dim() != 2:
+    if bounds.dim() == 0:
         raise ValueError("bounds must be [num_pages][dora_page_bounds_bytes]")
     stride, budget = block_table.shape[1], page_lists.shape[2]
     desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,

@@ -681,9 +681,10 @@ def _capturing(torch, stream):
 
 def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, workspace):
     """_call with a workspace of bytes_fn(args[0], *sizes) bytes after args (its size goes by the
-    device's compute units).  Without one given, the cached one of (thread, device, stream): two
-    threads' calls, of two launches each, may take turns on one stream.  While a graph is captured
-    a new one, from the graph's own memory, so that no two graphs share one."""
+    device's compute units), or of bytes_fn bytes where that is a number.  Without one given, the
+    cached one of (thread, device, stream): two threads' calls, of two launches each, may take turns
+    on one stream.  While a graph is captured a new one, from the graph's own memory, so that no two
+    graphs share one."""
     torch = _torch()
     if torch._C._cuda_getDevice() != device.index:
         with torch.cuda.device(device):
@@ -701,7 +702,7 @@ def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, workspace
         st = getattr(_lib, where)(*args, workspace.data_ptr(), workspace.numel(), handle)
         if st != DORA_ERR_WORKSPACE_TOO_SMALL:
             return _check(st, where)
-    need = int(getattr(_lib, bytes_fn)(args[0], *sizes))
+    need = bytes_fn if type(bytes_fn) is int else int(getattr(_lib, bytes_fn)(args[0], *sizes))
     if need == 0:  # invalid or unsupported: let the library name the reason
         return _call(device, stream, where, (*args, None, 0))
     if capturing:
@@ -1031,7 +1032,7 @@ def dora_page_select(q, bounds, block_table, seq_lens, page_lists, page_counts, 
     _call_with_workspace(q.device, stream, "dora_page_select",
                          (ctypes.byref(desc), budget, _i32("sink_pages", sink_pages),
                           _i32("recent_pages", recent_pages), *ptrs[:8]),
-                         "dora_page_select_workspace_bytes", (), workspace)
+                         "dora_page_select_workspace_bytes" if scores is None else 256, (), workspace)
 
 
 def dora_decode_pages_workspace_bytes(desc: dora_decode_desc, list_stride) -> int:

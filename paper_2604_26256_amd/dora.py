@@ -321,6 +321,33 @@ def dora_decode_segment_pages(desc: dora_decode_desc) -> int:
 _ws_cache = {}
 
 
+def _capturing(torch, stream):
+    c = torch._C
+    if stream is None:
+        return c._cuda_isCurrentStreamCapturing()
+    if stream.device_index != c._cuda_getDevice():
+        with torch.cuda.stream(stream):
+            return c._cuda_isCurrentStreamCapturing()
+    # (torch.cuda.stream takes 6 us, this 1)
+    was = c._cuda_getCurrentStream(stream.device_index)
+    c._cuda_setStream(stream_id=stream.stream_id, device_index=stream.device_index,
+                      device_type=stream.device_type)
+    try:
+        return c._cuda_isCurrentStreamCapturing()
+    finally:
+        c._cuda_setStream(stream_id=was[0], device_index=was[1], device_type=was[2])
+
+
+def _decode_workspace(cache, device, stream, need):
+    """The cached workspace; while a graph is captured a new one, from the graph's own memory:
+    graphs captured on one stream may be replayed at once on others, and beside its eager calls."""
+    torch = _torch()
+    if not _capturing(torch, stream):
+        return _cached_workspace(cache, device, stream, need)
+    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+
+
 def _cached_workspace(cache, device, stream, need):
     key = (device.index, _stream_handle(stream, device))
     ws = cache.get(key)
@@ -381,7 +408,7 @@ def dora_decode_attn(q, k_pages, v_pages, block_table, seq_lens, version_ids, ou
     version_ids int32 [B].  num_waves / min_range_pages override how the
     work is cut (0 = library default).  stream: a torch stream (default: the
     current one).  The workspace is allocated when not given (cached per
-    device and stream).  events: three raw hipEvent_t handles, which selects
+    device and stream; a captured call's is its own).  events: three raw hipEvent_t handles, which selects
     dora_decode_attn_timed (include/dora_measure.h).  Returns `out`.
     """
     desc, args = _decode_args(q, k_pages, v_pages, block_table, seq_lens, version_ids, out,
@@ -397,7 +424,7 @@ def dora_decode_attn(q, k_pages, v_pages, block_table, seq_lens, version_ids, ou
         _check(_lib.dora_decode_attn(ctypes.byref(desc), *args, None, 0,
                                      _stream_handle(stream)), "dora_decode_attn")
     if workspace is None:
-        workspace = _cached_workspace(_ws_cache, q.device, stream, need)
+        workspace = _decode_workspace(_ws_cache, q.device, stream, need)
     ws_ptr = _dev_ptr(workspace, "workspace", (_torch().uint8,))
     if events is None:
         st = _lib.dora_decode_attn(ctypes.byref(desc), *args, ws_ptr, workspace.numel(),
@@ -555,7 +582,7 @@ def dora_decode_attn_grouped(q, k_pages, v_pages, block_table, seq_lens, version
                                              _stream_handle(stream)),
                "dora_decode_attn_grouped")
     if workspace is None:
-        workspace = _cached_workspace(_gws_cache, q.device, stream, need)
+        workspace = _decode_workspace(_gws_cache, q.device, stream, need)
     st = _lib.dora_decode_attn_grouped(ctypes.byref(desc), *args,
                                        _dev_ptr(workspace, "workspace", (torch.uint8,)),
                                        workspace.numel(), _stream_handle(stream))
@@ -670,13 +697,6 @@ def _call(device, stream, where, args):
 
 
 _thread = threading.local()  # workspaces of this thread's calls, by the call's name
-
-
-def _capturing(torch, stream):
-    if stream is None:
-        return torch._C._cuda_isCurrentStreamCapturing()
-    with torch.cuda.stream(stream):
-        return torch.cuda.is_current_stream_capturing()
 
 
 def _call_with_workspace(device, stream, where, args, bytes_fn, sizes, workspace):

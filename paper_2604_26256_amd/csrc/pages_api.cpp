@@ -141,9 +141,8 @@ dora_status dora_decode_attn_pages(const dora_decode_desc* desc, int32_t list_st
     p.list_stride = list_stride;
     p.chunk_pages = w.chunk_pages;
     p.chunks = w.chunks;
-    p.waves = w.chunks > 1 ? kSegWaves
-                           : pages_waves(d, (int64_t)p.num_seqs * d.num_kv_heads,
-                                         (int64_t)list_stride * d.page_size);
+    p.waves = pages_waves(d, w.chunks, (int64_t)p.num_seqs * d.num_kv_heads,
+                          (int64_t)list_stride * d.page_size);
     p.scale_log2 = scale_log2_of(d);
     if (launch_pages(p, d.kv_dtype, s) != hipSuccess) return DORA_ERR_HIP;
     if (p.chunks > 1 && launch_pages_combine(p, s) != hipSuccess) return DORA_ERR_HIP;

@@ -75,13 +75,15 @@ inline void pages_layout(const dora_decode_desc& d, int32_t list_stride, PagesLa
   w->total = up(w->part_ml_off + slots * G * 8);
 }
 
-// Waves of a workgroup that has a whole list of at most `tokens`.  With one, four times as many lists are
+// Waves of a workgroup: four where a list is cut into chunks, else as many as a whole list of at most
+// `tokens` wants.  With one, four times as many lists are
 // under way and none is merged, but a list's steps follow each other: so for short lists of many
 // segments, and of 4-bit pages (64 tokens a step) for all where the segments are two to a CU.
 // Over 1,090 drawn batches of lists of 16 to 4,096 tokens this takes 1.01 of the better one's time,
 // four waves always 1.16 for 4-bit pages, 1.07 for bf16 and 1.06 for fp8 (8,000 4-bit lists of 32
 // tokens: 47 and 21 us; 1,024 of 2,560: 75.8 and 69.8; 4,000 fp8 lists of up to 3,200: 434 and 480).
-inline int pages_waves(const dora_decode_desc& d, int64_t segs, int64_t tokens) {
+inline int pages_waves(const dora_decode_desc& d, int chunks, int64_t segs, int64_t tokens) {
+  if (chunks > 1) return kSegWaves;
   const bool one = d.kv_dtype == DORA_KV_FP4
                        ? (tokens <= 64 && segs >= 128) || (tokens <= 4096 && segs >= 512)
                        : (tokens <= 32 && segs >= 128) || (tokens <= 256 && segs >= 640);

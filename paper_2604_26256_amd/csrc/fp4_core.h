@@ -27,7 +27,6 @@
 namespace dora {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kFp4Step = 64;  // tokens
 

@@ -71,12 +71,9 @@ PathParams last_tokens(const dora_decode_desc& d, int32_t num_tokens, const int3
   return p;
 }
 
-dora_status check_last(const dora_decode_desc& d, int32_t num_tokens) {
-  (void)d;
+dora_status check_last(int32_t num_tokens) {
   return num_tokens < 1 || num_tokens > DORA_PATH_MAX_TOKENS ? DORA_ERR_INVALID_ARG : DORA_OK;
 }
-
-size_t scores_off() { return kWsHeaderBytes; }
 
 }  // namespace
 
@@ -163,7 +160,7 @@ dora_status dora_kv_page_bounds(const dora_decode_desc* desc, int32_t num_tokens
   dora_status st = check_desc(desc);
   if (st != DORA_OK) return st;
   const dora_decode_desc& d = *desc;
-  st = check_last(d, num_tokens);
+  st = check_last(num_tokens);
   if (st != DORA_OK) return st;
   if (d.num_seqs == 0) return DORA_OK;
   if (!k_pages || !block_table || !seq_lens || !bounds) return DORA_ERR_INVALID_ARG;
@@ -181,7 +178,7 @@ dora_status dora_kv_page_bounds(const dora_decode_desc* desc, int32_t num_tokens
 size_t dora_page_select_workspace_bytes(const dora_decode_desc* desc) {
   if (check_desc(desc) != DORA_OK) return 0;
   const int seqs = desc->num_seqs < kMaxSeqsPerLaunch ? desc->num_seqs : kMaxSeqsPerLaunch;
-  return scores_off() + (size_t)seqs * desc->num_kv_heads * desc->block_table_stride * 4;
+  return kWsHeaderBytes + (size_t)seqs * desc->num_kv_heads * desc->block_table_stride * 4;
 }
 
 dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32_t sink_pages,
@@ -200,7 +197,7 @@ dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32
     return DORA_ERR_INVALID_ARG;
   if ((d.flags & DORA_FLAG_VALIDATE) && !version_ids && d.page_owner) return DORA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(bounds) || !aligned16(workspace)) return DORA_ERR_INVALID_ARG;
-  if (workspace_bytes < (scores ? scores_off() : dora_page_select_workspace_bytes(desc)))
+  if (workspace_bytes < (scores ? kWsHeaderBytes : dora_page_select_workspace_bytes(desc)))
     return DORA_ERR_WORKSPACE_TOO_SMALL;
   hipStream_t s = (hipStream_t)stream;
   uint8_t* ws = (uint8_t*)workspace;
@@ -216,7 +213,7 @@ dora_status dora_page_select(const dora_decode_desc* desc, int32_t budget, int32
     p.bounds = (const uint8_t*)bounds;
     p.block_table = block_table + (int64_t)c0 * d.block_table_stride;
     p.seq_lens = seq_lens + c0;
-    p.scores = scores ? scores + seg0 * d.block_table_stride : (float*)(ws + scores_off());
+    p.scores = scores ? scores + seg0 * d.block_table_stride : (float*)(ws + kWsHeaderBytes);
     p.lists = page_lists + seg0 * budget;
     p.counts = page_counts + seg0;
     p.record = bounds_bytes(d.num_kv_heads, d.head_dim);
@@ -248,7 +245,7 @@ dora_status dora_kv_read(const dora_decode_desc* desc, int32_t num_tokens, const
   dora_status st = check_desc(desc);
   if (st != DORA_OK) return st;
   const dora_decode_desc& d = *desc;
-  st = check_last(d, num_tokens);
+  st = check_last(num_tokens);
   if (st != DORA_OK) return st;
   if (d.num_seqs == 0) return DORA_OK;
   if (!k_pages || !v_pages || !block_table || !seq_lens || !k_out || !v_out)

@@ -425,9 +425,11 @@ size_t dora_page_bounds_bytes(int32_t num_kv_heads, int32_t head_dim);
  *   s = max(max |x| / 127, 2^-126), largest[d] = ceil(max x_d / s), smallest[d] =
  *   floor(min x_d / s), within +-127
  * where a NaN (of 4-bit pages, a NaN block) counts as 0 and an infinity as bf16's largest
- * number.  A page's bounds follow from its keys alone: those of a copied page may be copied
- * with it or taken again, those of a page that is given to another sequence are taken
- * as its tokens are appended.
+ * number.  The calls that move pages (dora_kv_page_copy, pack, unpack) leave bounds to the
+ * caller: records of pages that dora_pool_compact or a migration moves whole are copied with
+ * them, or taken again; a fork's own page, which may hold fewer tokens than the page it was
+ * copied from, has its bounds taken again; those of a page that is given to another
+ * sequence are taken as its tokens are appended.
  *   num_tokens   in [1, DORA_PATH_MAX_TOKENS]
  *   bounds       device [num_pages] records of dora_page_bounds_bytes, 16-byte aligned
  *   dev_status   as for dora_kv_append_path; a page that is skipped keeps its bounds

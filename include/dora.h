@@ -447,7 +447,8 @@ dora_status dora_kv_page_bounds(const dora_decode_desc* desc, int32_t num_tokens
  *   s * max over the group's rows h of fp32(r_h * sum_d max(u_hd lo_d, u_hd hi_d))
  * with hi, lo, s the page's bounds and the row as whole numbers u_hd = rint(q_hd / r_h), r_h
  * = max(max |q_h| / 127, 2^-126): each operation in fp32 with IEEE rounding, the sum exact.
- * So the choice depends on nothing but its inputs.  A NaN of q counts as 0.
+ * So the choice depends on nothing but its inputs.  A NaN of q counts as 0, an infinity as
+ * bf16's largest number.
  *   desc         num_seqs, heads, head_dim, page_size, block_table_stride, num_pages;
  *                kv_dtype and scales are not used; DORA_FLAG_VALIDATE checks the tables
  *   budget       pages of a list, >= max(1, sink_pages + recent_pages), < 2^19

@@ -404,7 +404,8 @@ def dora_decode_attn(q, k_pages, v_pages, block_table, seq_lens, version_ids, ou
 
     q, out: bf16 [B][Hq][d]; k_pages: [num_pages][Hkv][d/X][P][X]; v_pages:
     [num_pages][Hkv][d][P] (bf16, or uint8 / float8_e4m3fn codes with fp32
-    k_scales / v_scales [num_pages]); block_table int32 [B][stride]; seq_lens,
+    k_scales / v_scales [num_pages]; of 4-bit pages both uint8 [num_pages][Hkv][P * d * 17 / 32],
+    scales among them); block_table int32 [B][stride]; seq_lens,
     version_ids int32 [B].  num_waves / min_range_pages override how the
     work is cut (0 = library default).  stream: a torch stream (default: the
     current one).  The workspace is allocated when not given (cached per

@@ -321,29 +321,28 @@ def dora_decode_segment_pages(desc: dora_decode_desc) -> int:
 _ws_cache = {}
 
 
+# The HIP runtime's own question whether a stream is captured, which the library is linked with: 0.4 us of
+# a given stream, 6 by torch.cuda.stream and torch's.
+_lib.hipStreamIsCapturing.argtypes = [_P, _P]
+_lib.hipStreamIsCapturing.restype = ctypes.c_int
+
+
 def _capturing(torch, stream):
-    c = torch._C
     if stream is None:
-        return c._cuda_isCurrentStreamCapturing()
-    if stream.device_index != c._cuda_getDevice():
-        with torch.cuda.stream(stream):
-            return c._cuda_isCurrentStreamCapturing()
-    # (torch.cuda.stream takes 6 us, this 1)
-    was = c._cuda_getCurrentStream(stream.device_index)
-    c._cuda_setStream(stream_id=stream.stream_id, device_index=stream.device_index,
-                      device_type=stream.device_type)
-    try:
-        return c._cuda_isCurrentStreamCapturing()
-    finally:
-        c._cuda_setStream(stream_id=was[0], device_index=was[1], device_type=was[2])
+        return torch._C._cuda_isCurrentStreamCapturing()
+    status = ctypes.c_int()
+    _lib.hipStreamIsCapturing(stream.cuda_stream, ctypes.byref(status))
+    return status.value != 0
 
 
-def _decode_workspace(cache, device, stream, need):
+def _decode_workspace(cache, device, stream, handle, need):
     """The cached workspace; while a graph is captured a new one, from the graph's own memory:
     graphs captured on one stream may be replayed at once on others, and beside its eager calls."""
     torch = _torch()
     if not _capturing(torch, stream):
-        return _cached_workspace(cache, device, stream, need)
+        ws = cache.get((device.index, handle))
+        return (ws if ws is not None and ws.numel() == need
+                else _cached_workspace(cache, device, stream, need))
     with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
         return torch.empty(need, dtype=torch.uint8, device=device)
 
@@ -365,11 +364,11 @@ def _decode_args(q, k_pages, v_pages, block_table, seq_lens, version_ids, out, *
                  page_size, kv_dtype, sm_scale, k_scales, v_scales, page_owner, flags,
                  num_waves, min_range_pages):
     torch = _torch()
-    B, Hq, D = (int(x) for x in q.shape)
+    B, Hq, D = q.shape
     num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B][stride]")
-    stride = int(block_table.shape[1])
+    stride = block_table.shape[1]
     desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
                             page_size=page_size, block_table_stride=max(1, stride),
                             num_pages=num_pages, kv_dtype=kv_dtype, sm_scale=sm_scale,
@@ -424,19 +423,21 @@ def dora_decode_attn(q, k_pages, v_pages, block_table, seq_lens, version_ids, ou
         # invalid or unsupported geometry: let the library name the reason
         _check(_lib.dora_decode_attn(ctypes.byref(desc), *args, None, 0,
                                      _stream_handle(stream)), "dora_decode_attn")
+    handle = _stream_handle(stream)
     if workspace is None:
-        workspace = _decode_workspace(_ws_cache, q.device, stream, need)
-    ws_ptr = _dev_ptr(workspace, "workspace", (_torch().uint8,))
+        workspace = _decode_workspace(_ws_cache, q.device, stream, handle, need)
+        ws_ptr = workspace.data_ptr()
+    else:
+        ws_ptr = _dev_ptr(workspace, "workspace", (_torch().uint8,))
     if events is None:
-        st = _lib.dora_decode_attn(ctypes.byref(desc), *args, ws_ptr, workspace.numel(),
-                                   _stream_handle(stream))
+        st = _lib.dora_decode_attn(ctypes.byref(desc), *args, ws_ptr, workspace.numel(), handle)
         _check(st, "dora_decode_attn")
     else:
         if len(events) != 3:
             raise ValueError("events needs 3 hipEvent_t handles")
         arr = (ctypes.c_void_p * 3)(*[ctypes.c_void_p(e) for e in events])
         st = _lib.dora_decode_attn_timed(ctypes.byref(desc), *args, ws_ptr, workspace.numel(),
-                                         _stream_handle(stream), ctypes.cast(arr, _P))
+                                         handle, ctypes.cast(arr, _P))
         _check(st, "dora_decode_attn_timed")
     return out
 
@@ -549,11 +550,11 @@ def dora_decode_attn_grouped(q, k_pages, v_pages, block_table, seq_lens, version
     once per group.  shared_pages_out: optional device int32 [B / group_size]
     that receives each group's shared page count.  See include/dora.h."""
     torch = _torch()
-    B, Hq, D = (int(x) for x in q.shape)
+    B, Hq, D = q.shape
     num_pages, kv_types = _kv_geometry(k_pages, v_pages, num_kv_heads, page_size, D, kv_dtype)
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise ValueError("block_table must be [B][stride]")
-    stride = int(block_table.shape[1])
+    stride = block_table.shape[1]
     desc = make_decode_desc(num_seqs=B, num_q_heads=Hq, num_kv_heads=num_kv_heads, head_dim=D,
                             page_size=page_size, block_table_stride=max(1, stride),
                             num_pages=num_pages, kv_dtype=kv_dtype, sm_scale=sm_scale,
@@ -582,11 +583,13 @@ def dora_decode_attn_grouped(q, k_pages, v_pages, block_table, seq_lens, version
         _check(_lib.dora_decode_attn_grouped(ctypes.byref(desc), *args, None, 0,
                                              _stream_handle(stream)),
                "dora_decode_attn_grouped")
+    handle = _stream_handle(stream)
     if workspace is None:
-        workspace = _decode_workspace(_gws_cache, q.device, stream, need)
-    st = _lib.dora_decode_attn_grouped(ctypes.byref(desc), *args,
-                                       _dev_ptr(workspace, "workspace", (torch.uint8,)),
-                                       workspace.numel(), _stream_handle(stream))
+        workspace = _decode_workspace(_gws_cache, q.device, stream, handle, need)
+        ws_ptr = workspace.data_ptr()
+    else:
+        ws_ptr = _dev_ptr(workspace, "workspace", (torch.uint8,))
+    st = _lib.dora_decode_attn_grouped(ctypes.byref(desc), *args, ws_ptr, workspace.numel(), handle)
     _check(st, "dora_decode_attn_grouped")
     return out
 

@@ -2,11 +2,12 @@
 // names, or, of 4-bit pages without lists, all pages of a short row.
 //
 // Bound by memory: each listed page is read once, by one wave, straight into matrix operands
-// (16 query columns: a KV head's group), two steps of loads in flight.  512 lists of 2,048 tokens in
-// bf16 (537 MB) take 86 us, 6.2 TB/s; 4,000 fp8 lists of up to 3,200 tokens (2.65 GB) 434 us, 6.1; 1,024
-// 4-bit lists of 2,560 tokens in pages of 16 (347 MB) 70 us, 4.9, where pages of 32 reach 5.5: a 4-bit
-// tile of 16 tokens and 128 dims is 1,088 bytes, half a line more than whole ones, and the rate of
-// tiles read here and there falls with their size.  Reading lists beside lengths and counts, one wait
+// (16 query columns: a KV head's group), two steps of loads in flight.  In a stream of calls, where one's start
+// covers the other's end, 512 lists of 2,048 tokens in bf16 (537 MB) take 86 us, 6.2 TB/s (89 to 93 in
+// a trace, which runs kernels one by one); 4,000 fp8 lists of up to 3,200 tokens (2.65 GB) 433 us, 6.1; 1,024
+// 4-bit lists of 2,560 tokens of 128 dims in pages of 16 (347 MB) 70 us, 4.9 (72 to 75), where pages of 32
+// take 59, 5.8: a tile of 16 such tokens is 1,088 bytes, half a line more than whole ones, and the rate
+// of tiles read here and there falls with their size.  Reading lists beside lengths and counts, one wait
 // fewer at the start, changed nothing: what runs beside a start hides it.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -194,7 +194,7 @@ int64_t dora_decode_num_waves(const dora_decode_desc* desc);
  * from 768 tokens on); dora_decode_segment_pages in dora_measure.h tells which.
  * Results do not depend on the number of wavefronts beyond fp32 rounding, and
  * repeated calls on the same inputs and device are bitwise identical.
- * Scores and sums are held in fp32.  Of 4-bit pages any finite values give a finite
+ * Scores and sums are held in fp32.  Of 4-bit pages values of up to 2^127 give a finite
  * result; of bf16 and fp8 pages the magnitudes of the values that a row attends, each
  * times its weight relative to the row's largest, have to add up to less than 2^128. */
 dora_status dora_decode_attn(const dora_decode_desc* desc,
